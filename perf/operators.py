@@ -16,7 +16,7 @@ import torch
 own = False
 
 BLOCK = 16
-TOP_SCALE = 0xE1     # largest scale a block gets: 7 * scale stays a finite half-precision number
+TOP_SCALE = 0xC6     # largest scale a block gets (896): 72 * scale stays a finite half-precision number
 NAN_SCALE = 0xFF     # a block that held an infinity or NaN
 
 
