@@ -18,7 +18,8 @@
  *   - Matrices are row-major [out_features, in_features] in the model dtype
  *     (CLASP_BF16: bfloat16, CLASP_FP32: float).  Norm weights are float.
  *   - The KV cache of one layer is two arrays [max_ctx, n_kv_heads, head_dim] in
- *     the model dtype; keys are stored AFTER rotary embedding.
+ *     the model dtype; keys are stored AFTER rotary embedding.  (Contexts made with
+ *     CLASP_FLAG_KV4: two packed arrays, see clasp_kv4_bytes.)
  *   - Hidden states / residual stream are float everywhere.
  *   - Layers are f_0..f_{L-1};  h_0 = embedding,  h_{l+1} = f_l(h_l)  (Sec. 3.4).
  *   - Every function returns CLASP_OK (0) or a negative CLASP_ERR_*; nothing
@@ -100,6 +101,8 @@ typedef struct clasp_config {
                                    when it serves 256 or more) keep the attention over the cache keys on the warp-level multiply
                                    instead of tcgen05 (the two sum a row's keys in different orders:
                                    results agree to rounding, not bit for bit) */
+
+#define CLASP_FLAG_KV4 32 /* the context's KV cache is held in 4 bits: see clasp_kv4_bytes */
 
 /* Device pointers to the nine tensors of one decoder layer (borrowed). */
 typedef struct clasp_layer_weights {
@@ -276,6 +279,48 @@ int clasp_accept(const int32_t* draft, const int32_t* full_argmax, int32_t K,
 int clasp_layer_forward(clasp_ctx* ctx, int32_t layer, const float* x_in, int64_t in_stride,
                         int32_t S, int32_t T, int32_t ctx_len, int32_t pos0,
                         const clasp_kv_layer* kv_layer, int32_t write_kv, float* x_out,
+                        int64_t out_stride);
+
+/* ---- KV cache held in 4 bits (no counterpart in the paper; for contexts whose bf16 cache would not fit, or would
+ * cost more to read per token than the weights).  A context made with CLASP_FLAG_KV4 has such a cache: every call above
+ * that takes clasp_kv_layer then takes packed arrays, 9/32 of the bytes of a bf16 cache, and new keys and values are
+ * quantised before the rows attend to them (so verification and one-token decoding see the same cache).  Its calls run
+ * one kernel per step.
+ *
+ * Format.  A block is 16 consecutive dims of one position's key or value, sixteen 4-bit codes c and one scale byte b:
+ *     value = (c - 8) * s,   s = the half-precision number with the bits b << 7
+ * Written: s the smallest such number with 7 s >= the block's largest magnitude (at most 896: magnitudes above 6272
+ * saturate), c - 8 = x / s to the nearest, ties to even.  A block that holds an infinity or NaN gets b = 0xFF and reads
+ * back as NaN throughout.  The bytes are a function of the row alone; every value is exact in bf16.  The array of one
+ * layer's keys (or values): codes [n_kv_heads, max_ctx, head_dim / 2], low nibble first, then scale bytes
+ * [n_kv_heads, max_ctx, head_dim / 16]; 16-byte aligned.  max_ctx is at most 2^30.
+ *
+ * The calls below need a context made with CLASP_FLAG_KV4 and its device current, run on its stream and use its
+ * workspace (calls, and captured graphs of calls, on one context must not overlap on the GPU).  Rows of heads are in the
+ * model dtype, head_dim elements per head, heads of a row contiguous; pointers 16-byte aligned, strides in elements, at
+ * least a row and a multiple of 16 bytes.  Zero rows are no error and launch nothing.
+ * Errors: INVALID_ARG, CAPACITY (positions past max_ctx, more than max_rows rows of queries). */
+
+/* Bytes of one layer's packed keys (or values); 0 when the configuration is bad or lacks CLASP_FLAG_KV4.  Host-only. */
+size_t clasp_kv4_bytes(const clasp_config* cfg);
+
+/* Rows k, v [n, n_kv_heads, head_dim] (keys after rotary embedding) into positions pos0..pos0+n-1 of a layer. */
+int clasp_kv4_write(clasp_ctx* ctx, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n,
+                    int32_t pos0, const clasp_kv_layer* kv_layer);
+
+/* Positions pos0..pos0+n-1 of a layer as rows in the model dtype. */
+int clasp_kv4_read(clasp_ctx* ctx, const clasp_kv_layer* kv_layer, int32_t pos0, int32_t n, void* k_out, int64_t k_stride,
+                   void* v_out, int64_t v_stride);
+
+/* softmax(q k^T / sqrt(head_dim)) v of S states of T rows (row s*T + t) over a layer's cache.  Every row sees positions
+ * [0, ctx_len); with `visible` (device int32[S*T], or NULL) row r sees min(ctx_len, max(0, visible[r])) of them, read when
+ * the kernel runs, so a captured call follows it.  With own_pos0 >= 0 a row also sees the rows of its own state up to
+ * itself, whose keys and values lie at positions own_pos0 + s*T + t (written before; own_pos0 == ctx_len with S == 1 is a
+ * verification); own_pos0 == -1: none.  A row that sees nothing gives zeros; a NaN block reaches the rows that see it and no
+ * others.  Scores must be finite in fp32.  q, out: [S*T, n_q_heads, head_dim]; they must not overlap.
+ * A row's result does not depend on the rows that share the call. */
+int clasp_kv4_attention(clasp_ctx* ctx, const void* q, int64_t q_stride, int32_t S, int32_t T, int32_t ctx_len,
+                        int32_t own_pos0, const int32_t* visible, const clasp_kv_layer* kv_layer, void* out,
                         int64_t out_stride);
 
 /* y[r, n] = sum_k x[r, k] * w[n, k]  (float out) through the same weight-

@@ -18,11 +18,13 @@ from . import build as _build
 CLASP_FP32, CLASP_BF16 = 0, 1
 CHOICE_APPLY, CHOICE_SKIP, CHOICE_NONE = 0, 1, 255
 FLAG_FORCE_SIMT, FLAG_NO_DEFER, FLAG_MULTI_KERNEL, FLAG_PRUNE, FLAG_NO_ATT_TC = 1, 2, 4, 8, 16
+FLAG_KV4 = 32
 
 SYMBOLS = ["clasp_workspace_bytes", "clasp_create", "clasp_destroy", "clasp_load_layers", "clasp_load_head",
            "clasp_dp_search", "clasp_verify", "clasp_draft_forward", "clasp_accept", "clasp_layer_forward",
            "clasp_gemm_xwT", "clasp_gemm_xwT_noalloc", "clasp_profile_gemm", "clasp_last_device_status", "clasp_launch_count", "clasp_engine_trace", "clasp_strerror",
-           "clasp_engine_active", "clasp_set_wait_limit", "clasp_draft_sample", "clasp_verify_sample"]
+           "clasp_engine_active", "clasp_set_wait_limit", "clasp_draft_sample", "clasp_verify_sample",
+           "clasp_kv4_bytes", "clasp_kv4_write", "clasp_kv4_read", "clasp_kv4_attention"]
 
 
 class ClaspConfig(C.Structure):
@@ -103,6 +105,14 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.clasp_engine_active.argtypes = [vp]
     lib.clasp_set_wait_limit.restype = C.c_int
     lib.clasp_set_wait_limit.argtypes = [vp, C.c_uint32]
+    lib.clasp_kv4_bytes.restype = C.c_size_t
+    lib.clasp_kv4_bytes.argtypes = [C.POINTER(ClaspConfig)]
+    lib.clasp_kv4_write.restype = C.c_int
+    lib.clasp_kv4_write.argtypes = [vp, vp, i64, vp, i64, i32, i32, C.POINTER(ClaspKvLayer)]
+    lib.clasp_kv4_read.restype = C.c_int
+    lib.clasp_kv4_read.argtypes = [vp, C.POINTER(ClaspKvLayer), i32, i32, vp, i64, vp, i64]
+    lib.clasp_kv4_attention.restype = C.c_int
+    lib.clasp_kv4_attention.argtypes = [vp, vp, i64, i32, i32, i32, i32, vp, C.POINTER(ClaspKvLayer), vp, i64]
     lib.clasp_strerror.restype = C.c_char_p
     lib.clasp_strerror.argtypes = [C.c_int]
     _lib = lib
@@ -160,6 +170,24 @@ class KVCache:
             self.array[l].v = self.v[l].data_ptr()
 
 
+class KV4Cache:
+    """Device KV cache of a context made with FLAG_KV4: per layer the packed keys and values (4-bit codes, then one scale byte
+    per 16 dims).  Takes the place of KVCache in every call of such a context."""
+
+    def __init__(self, cfg: ClaspConfig, device="cuda"):
+        nbytes = load_library().clasp_kv4_bytes(C.byref(cfg))
+        if nbytes == 0:
+            raise ClaspError(-2, "clasp_kv4_bytes")
+        # zero bytes read back as zeros: scale 0.  A layer's array starts on a 16-byte boundary.
+        self.k, self.v = (torch.zeros((cfg.L, (nbytes + 15) // 16 * 16), dtype=torch.uint8, device=device)[:, :nbytes]
+                          for _ in range(2))
+        self.array = (ClaspKvLayer * cfg.L)()
+        for l in range(cfg.L):
+            self.array[l].k = self.k[l].data_ptr()
+            self.array[l].v = self.v[l].data_ptr()
+        self.layers = [C.pointer(self.array[l]) for l in range(cfg.L)]
+
+
 class Clasp:
     """Owns a clasp_ctx, its workspace and references to the borrowed weights."""
 
@@ -169,6 +197,7 @@ class Clasp:
         self.lib = load_library()
         self.cfg = cfg
         self.device = torch.device(device)
+        self.dtype = torch.bfloat16 if cfg.dtype == CLASP_BF16 else torch.float32
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         nbytes = self.lib.clasp_workspace_bytes(C.byref(cfg))
         if nbytes == 0:
@@ -284,6 +313,87 @@ class Clasp:
         _check(self.lib.clasp_gemm_xwT(self.handle, x.data_ptr(), w.data_ptr(), R, N, K, y.data_ptr()),
                "clasp_gemm_xwT")
         return y
+
+    # ---- cache held in 4 bits (contexts made with FLAG_KV4)
+    def _head_rows(self, t: torch.Tensor, heads: int, what: str) -> int:
+        """Stride in elements of rows [n, heads, head_dim] in the model dtype; the heads of a row are contiguous."""
+        hd = self.cfg.head_dim
+        if t.dtype != self.dtype or t.device != self.workspace.device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != hd:
+            raise ValueError(f"{what}: [n, {heads}, {hd}] {self.dtype} on {self.workspace.device} expected")
+        sr, sh, sd = t.stride()
+        if (sd != 1 or (sh != hd and heads > 1)) and t.shape[0]:
+            raise ValueError(f"{what}: the heads of a row must be contiguous")
+        return sr if t.shape[0] > 1 else max(sr, heads * hd)
+
+    def _new_rows(self, *shape: int) -> torch.Tensor:
+        t = torch.empty(shape, dtype=self.dtype, device=self.workspace.device)
+        # memory handed out for another stream than the one that fills it
+        if torch._C._cuda_getCurrentRawStream(self.workspace.device.index) != self.stream.cuda_stream:
+            t.record_stream(self.stream)
+        return t
+
+    @staticmethod
+    def _kv4_layer(kv: KV4Cache, layer: int):
+        if not isinstance(kv, KV4Cache):
+            raise ValueError("a KV4Cache is needed")
+        if not 0 <= layer < len(kv.layers):
+            raise ValueError(f"no layer {layer}")
+        return kv.layers[layer]
+
+    def kv4_write(self, k: torch.Tensor, v: torch.Tensor, pos0: int, kv: KV4Cache, layer: int = 0):
+        """Quantise rows k, v [n, n_kv_heads, head_dim] into positions pos0.. of one layer of a 4-bit cache."""
+        h = self.cfg.n_kv_heads
+        ks, vs = self._head_rows(k, h, "k"), self._head_rows(v, h, "v")
+        n = k.shape[0]
+        if v.shape[0] != n:
+            raise ValueError("k and v: as many rows")
+        _check(self.lib.clasp_kv4_write(self.handle, k.data_ptr(), ks, v.data_ptr(), vs, n, pos0, self._kv4_layer(kv, layer)),
+               "clasp_kv4_write")
+
+    def kv4_read(self, pos0: int, n: int, kv: KV4Cache, layer: int = 0, k_out: Optional[torch.Tensor] = None,
+                 v_out: Optional[torch.Tensor] = None):
+        """Rows pos0..pos0+n-1 of one layer of a 4-bit cache in the model dtype: (k, v), each [n, n_kv_heads, head_dim]."""
+        h = self.cfg.n_kv_heads
+        if n < 0:
+            raise ValueError("n: a number of rows")
+        if k_out is None and v_out is None:
+            k_out, v_out = self._new_rows(2, n, h, self.cfg.head_dim).unbind(0)
+        k_out = self._new_rows(n, h, self.cfg.head_dim) if k_out is None else k_out
+        v_out = self._new_rows(n, h, self.cfg.head_dim) if v_out is None else v_out
+        ks, vs = self._head_rows(k_out, h, "k_out"), self._head_rows(v_out, h, "v_out")
+        if k_out.shape[0] != n or v_out.shape[0] != n:
+            raise ValueError("k_out, v_out: n rows")
+        _check(self.lib.clasp_kv4_read(self.handle, self._kv4_layer(kv, layer), pos0, n, k_out.data_ptr(), ks, v_out.data_ptr(),
+                                       vs), "clasp_kv4_read")
+        return k_out, v_out
+
+    def kv4_attention(self, q: torch.Tensor, kv: KV4Cache, ctx_len: int, T: int = 1, own_pos0: Optional[int] = None,
+                      visible: Optional[torch.Tensor] = None, layer: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of q [S*T, n_q_heads, head_dim] (rotated queries, the T rows of a state together) over one layer of a 4-bit
+        cache.  Every row sees positions [0, ctx_len) -- with `visible` (int32 [S*T], device) row r only [0, visible[r]) of them
+        -- and, with own_pos0, the rows of its own state up to itself, whose keys and values lie at positions own_pos0 + row.  A
+        row that sees nothing gives zeros.  `out` must not overlap q."""
+        h = self.cfg.n_q_heads
+        qs = self._head_rows(q, h, "q")
+        R = q.shape[0]
+        if T < 1 or R % T:
+            raise ValueError("q: whole states of T rows")
+        if visible is not None and (visible.dtype != torch.int32 or visible.device != q.device or visible.shape != (R,)
+                                    or not visible.is_contiguous()):
+            raise ValueError(f"visible: int32 [{R}] on {q.device} expected")
+        if own_pos0 is None:
+            own_pos0 = -1
+        elif own_pos0 < 0:
+            raise ValueError("own_pos0: a position")
+        if out is None:
+            out, os = self._new_rows(R, h, self.cfg.head_dim), h * self.cfg.head_dim
+        else:
+            os = self._head_rows(out, h, "out")
+            if out.shape[0] != R:
+                raise ValueError("out: as many rows as q")
+        _check(self.lib.clasp_kv4_attention(self.handle, q.data_ptr(), qs, R // T, T, ctx_len, own_pos0, _ptr(visible),
+                                            self._kv4_layer(kv, layer), out.data_ptr(), os), "clasp_kv4_attention")
+        return out
 
     def device_status(self) -> int:
         return self.lib.clasp_last_device_status(self.handle)

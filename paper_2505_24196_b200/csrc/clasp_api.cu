@@ -1,7 +1,8 @@
 // C ABI of the layer-skip search library: context, argument checks and the host-side
 // launch sequences.  Every arithmetic step runs in a kernel -- engine2.cuh (bf16 calls of up
 // to 128 rows), wide.cuh (bf16 layers over more), small32.cuh (calls on small fp32 models),
-// kernels.cuh and gemm_tc.cuh (one kernel per step: everything else), sampling.cuh --; this
+// kernels.cuh and gemm_tc.cuh (one kernel per step: everything else), kv4.cuh (contexts whose
+// cache is held in 4 bits), sampling.cuh --; this
 // file only sequences launches on the caller's stream.
 #include "../../include/clasp.h"
 
@@ -22,6 +23,7 @@
 #include "gemm_tc.cuh"
 #include "kernels.cuh"
 #include "engine2.cuh"
+#include "kv4.cuh"
 #include "sampling.cuh"
 #include "small32.cuh"
 #include "wide.cuh"
@@ -37,6 +39,8 @@ using bf16 = __nv_bfloat16;
 constexpr int S32_MAX_KEYS = 2048;
 constexpr long long S32_MAX_SCORES = 65536;   // rows x query heads x keys
 constexpr int WIDE_MIN_ROWS = 128;   // layers over more rows take the products and the attention of wide.cuh
+constexpr int KV4_MAX_CTX = 1 << 30;   // positions of a 4-bit cache: key numbers and steps past the end stay in 32 bits
+constexpr int KV4_ROWS = 64;           // rows per launch of the attention of few rows: bounds its workspace
 constexpr int MAX_COUNTERS = 4096;   // tiles of one GEMM launch that may use split-K
 constexpr size_t PARTIAL_FLOATS = (size_t)296 * 2 * 128 * 128 + (1 << 20);
 
@@ -87,6 +91,11 @@ struct Workspace {
   clasp::pk::Job* jobs;
   int* tabs;
   clasp::smp::AcceptScratch* spec;
+  // 4-bit cache: partial results of the attention and arrival counters
+  float* kv4_part;
+  float2* kv4_ml;
+  int* kv4_counters;
+  size_t kv4_counter_bytes;
   int e_chunk_cap;
   int e_run_len;
   int e_rcap;
@@ -103,7 +112,22 @@ bool config_ok(const clasp_config* c) {
   if (c->vocab < 1 || c->max_ctx < 1 || c->max_rows < 1 || c->max_head_rows < 1) return false;
   if (c->max_M < 0 || c->max_M > c->L || c->max_T < 1) return false;
   if (c->dtype != CLASP_FP32 && c->dtype != CLASP_BF16) return false;
+  if ((c->flags & CLASP_FLAG_KV4) && c->max_ctx > KV4_MAX_CTX) return false;
   return true;
+}
+
+bool is_kv4(const clasp_config& c) { return (c.flags & CLASP_FLAG_KV4) != 0; }
+
+// Keys per run of the attention over a 4-bit cache.  A function of the capacity and the kv heads alone, so that verification
+// and one-token decoding sum a position's keys in the same order; at full capacity two CTAs per SM have a run.
+int kv4_run_len(const clasp_config& c) {
+  const int step = clasp::kv4::WARPS * clasp::kv4::STEP;
+  const int target = std::max(1, std::min(clasp::kv4::MAX_PARTS - 4, 2 * 148 / c.n_kv_heads));
+  return std::max(1, ((c.max_ctx + target - 1) / target + step - 1) / step) * step;
+}
+int kv4_max_parts(const clasp_config& c) {
+  const int len = kv4_run_len(c);
+  return (c.max_ctx + len - 1) / len + 1;
 }
 
 constexpr int ENGINE_MAX_CTAS = clasp::pk::MAX_CTAS;
@@ -139,12 +163,20 @@ Workspace carve(const clasp_config& c, uint8_t* base) {
   w.choice = (uint8_t*)take((size_t)(c.L + 1) * (c.max_M + 1));
   w.rope = (float2*)take(R * (c.head_dim / 2) * sizeof(float2));
   const size_t att_chunks = clasp::ATT_MAX_CACHE_CHUNKS + (R + clasp::ATT_KEYS - 1) / clasp::ATT_KEYS;
-  w.att_acc = (float*)take(R * c.n_q_heads * att_chunks * (size_t)c.head_dim * 4);
-  w.att_ml = (float2*)take(R * c.n_q_heads * att_chunks * sizeof(float2));
+  if (is_kv4(c)) {
+    const size_t slots = std::min(R, (size_t)KV4_ROWS) * c.n_q_heads * kv4_max_parts(c);
+    w.kv4_part = (float*)take(slots * c.head_dim * 4);
+    w.kv4_ml = (float2*)take(slots * sizeof(float2));
+    w.kv4_counter_bytes = (size_t)(KV4_ROWS * c.n_q_heads / 8 + c.n_kv_heads) * sizeof(int);
+    w.kv4_counters = (int*)take(w.kv4_counter_bytes);
+  } else {
+    w.att_acc = (float*)take(R * c.n_q_heads * att_chunks * (size_t)c.head_dim * 4);
+    w.att_ml = (float2*)take(R * c.n_q_heads * att_chunks * sizeof(float2));
+  }
   w.logits = (float*)take((size_t)c.max_head_rows * c.vocab * 4);
   w.partial = (float*)take(PARTIAL_FLOATS * 4);
   w.spec = (clasp::smp::AcceptScratch*)take(sizeof(clasp::smp::AcceptScratch));
-  if (c.dtype == CLASP_BF16) {
+  if (c.dtype == CLASP_BF16 && !is_kv4(c)) {
     // buffers of the persistent layer engine (per-CTA tables sized for ENGINE_MAX_CTAS)
     namespace pk = clasp::pk;
     const size_t Re = R < (size_t)pk::MAX_ROWS ? R : (size_t)pk::MAX_ROWS;
@@ -201,6 +233,7 @@ struct clasp_ctx {
   int cta_cap = 296;
   int smem_budget = 110 * 1024;
   int num_sms = 148;
+  int device = 0;
   bool use_s32 = false;     // fp32 model that fits one cluster's shared memory: one launch per call (small32.cuh)
   bool s32_head = false;    // ... and so does its LM head
   int s32_smem = 0;
@@ -543,6 +576,78 @@ int attention_wide(clasp_ctx* ctx, int R, int T, int C, const clasp_kv_layer& kv
   return launch_check(ctx);
 }
 
+// ---------------------------------------------------------------- cache in 4 bits (kv4.cuh)
+
+clasp::kv4::View kv4_view(const clasp_ctx* ctx, void* p, int64_t capacity) {
+  return clasp::kv4::view(p, ctx->cfg.n_kv_heads, ctx->cfg.head_dim, capacity);
+}
+
+template <int HD, bool SPLIT>
+int kv4_rows_launch(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
+  namespace k4 = clasp::kv4;
+  const int pairs = p.R * (p.nq / p.nkv);
+  // pairs per CTA: the fewest that hold them all, since every block of pairs reads the run again (SPLIT: the second operands
+  // take the registers of a third and fourth group)
+  const int nt = pairs <= 8 ? 1 : (pairs <= 16 || SPLIT) ? 2 : 4;
+  const dim3 grid(p.runs + (p.own_n > 0 ? 1 : 0), p.nkv, (pairs + 8 * nt - 1) / (8 * nt));
+  if (nt == 1) k4::attn_rows_kernel<HD, 1, SPLIT><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
+  else if (nt == 2) k4::attn_rows_kernel<HD, 2, SPLIT><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
+  else if constexpr (!SPLIT) k4::attn_rows_kernel<HD, 4, false><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
+  return launch_check(ctx);
+}
+
+// Attention of `p.R_all` rows described by p (q, out, views, masks) over the cache and the own rows.
+int kv4_attend(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
+  const clasp_config& c = ctx->cfg;
+  p.nq = c.n_q_heads;
+  p.nkv = c.n_kv_heads;
+  p.run_len = kv4_run_len(c);
+  p.runs = std::max(p.own_n > 0 ? 0 : 1, (p.n_keys + p.run_len - 1) / p.run_len);
+  p.part = ctx->ws.kv4_part;
+  p.part_ml = ctx->ws.kv4_ml;
+  p.counters = ctx->ws.kv4_counters;
+  const void* q = p.q;
+  void* out = p.out;
+  const bool split = c.dtype == CLASP_FP32;
+  for (int r0 = 0; r0 < p.R_all; r0 += KV4_ROWS) {
+    p.r0 = r0;
+    p.R = std::min(KV4_ROWS, p.R_all - r0);
+    p.q = (const char*)q + r0 * p.q_stride * (p.q_bf16 ? 2 : 4);
+    p.out = (char*)out + r0 * p.out_stride * (p.out_bf16 ? 2 : 4);
+    int rc;
+    if (c.head_dim == 128) rc = split ? kv4_rows_launch<128, true>(ctx, p) : kv4_rows_launch<128, false>(ctx, p);
+    else rc = split ? kv4_rows_launch<64, true>(ctx, p) : kv4_rows_launch<64, false>(ctx, p);
+    if (rc) return rc;
+  }
+  return CLASP_OK;
+}
+
+// Attention inside a layer: the rows' projections are in ws.qkv.  Their keys and values go to the cache at pos0 (write_kv) or
+// to scratch, quantised either way before the rows attend to them.
+int kv4_layer_attention(clasp_ctx* ctx, int S, int T, int C, int pos0, const clasp_kv_layer& kv, bool write_kv) {
+  namespace k4 = clasp::kv4;
+  const clasp_config& c = ctx->cfg;
+  Workspace& ws = ctx->ws;
+  const int R = S * T, qkvd = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
+  k4::AttnArgs p{};
+  p.k = kv4_view(ctx, kv.k, c.max_ctx);
+  p.v = kv4_view(ctx, kv.v, c.max_ctx);
+  p.own_k = write_kv ? p.k : kv4_view(ctx, ws.own_k, c.max_rows);
+  p.own_v = write_kv ? p.v : kv4_view(ctx, ws.own_v, c.max_rows);
+  p.own_pos0 = write_kv ? pos0 : 0;
+  const long long units = (long long)R * (qkvd / (2 * k4::BLOCK));
+  k4::store_rows_kernel<<<(unsigned)((units + 255) / 256), 256, 0, ctx->stream>>>(ws.qkv, qkvd, ws.rope, R, T, c.n_q_heads,
+                                                                                c.n_kv_heads, c.head_dim, p.own_k, p.own_v,
+                                                                                p.own_pos0);
+  int rc = launch_check(ctx);
+  if (rc) return rc;
+  p.q = ws.qkv; p.q_stride = qkvd; p.q_bf16 = 0;
+  p.out = ws.attn; p.out_stride = c.n_q_heads * c.head_dim; p.out_bf16 = c.dtype == CLASP_BF16;
+  p.R_all = R; p.T = T; p.n_keys = C; p.own_n = R;
+  if (write_kv && pos0 == C) { p.causal = 1; p.n_keys = C + R; p.own_n = 0; }
+  return kv4_attend(ctx, p);
+}
+
 template <typename TW>
 int rmsnorm(clasp_ctx* ctx, const float* x, int64_t ldx, const float* w, int R, void* y) {
   clasp::rmsnorm_kernel<TW><<<R, 256, 0, ctx->stream>>>(x, ldx, w, ctx->cfg.d_model, ctx->cfg.rms_eps, (TW*)y);
@@ -585,13 +690,17 @@ int run_layer(clasp_ctx* ctx, int l, const float* x, int64_t ldx, int S, int T, 
   TW* own_k = write_kv ? (TW*)kv.k : (TW*)ws.own_k;
   TW* own_v = write_kv ? (TW*)kv.v : (TW*)ws.own_v;
   const int64_t own_base = write_kv ? pos0 : 0;
-  clasp::kv_store_kernel<TW><<<R, 256, 0, ctx->stream>>>(ws.qkv, qkvd, ws.rope, T, c.n_q_heads, c.n_kv_heads,
-                                                         c.head_dim, own_k, own_v, own_base);
-  if ((rc = launch_check(ctx))) return rc;
-  if (wide && c.head_dim == clasp::wide::HD) rc = attention_wide(ctx, R, T, C, kv, (const bf16*)own_k, (const bf16*)own_v, own_base);
-  else if (c.head_dim == 128) rc = attention<TW, 128>(ctx, R, T, C, kv, own_k, own_v, own_base);
-  else rc = attention<TW, 64>(ctx, R, T, C, kv, own_k, own_v, own_base);
-  if (rc) return rc;
+  if (is_kv4(c)) {
+    if ((rc = kv4_layer_attention(ctx, S, T, C, pos0, kv, write_kv))) return rc;
+  } else {
+    clasp::kv_store_kernel<TW><<<R, 256, 0, ctx->stream>>>(ws.qkv, qkvd, ws.rope, T, c.n_q_heads, c.n_kv_heads,
+                                                           c.head_dim, own_k, own_v, own_base);
+    if ((rc = launch_check(ctx))) return rc;
+    if (wide && c.head_dim == clasp::wide::HD) rc = attention_wide(ctx, R, T, C, kv, (const bf16*)own_k, (const bf16*)own_v, own_base);
+    else if (c.head_dim == 128) rc = attention<TW, 128>(ctx, R, T, C, kv, own_k, own_v, own_base);
+    else rc = attention<TW, 64>(ctx, R, T, C, kv, own_k, own_v, own_base);
+    if (rc) return rc;
+  }
   {
     GemmCall g;
     g.x = ws.attn; g.R = R; g.K = qd; g.n_mats = 1; g.w[0] = W.wo; g.wide = wide;
@@ -694,7 +803,7 @@ int s32_launch_config(clasp_ctx* ctx, cudaLaunchConfig_t* lc, cudaLaunchAttribut
 int s32_setup(clasp_ctx* ctx) {
   const clasp_config& c = ctx->cfg;
   ctx->use_s32 = ctx->s32_head = false;
-  if (c.dtype != CLASP_FP32 || (c.flags & CLASP_FLAG_MULTI_KERNEL)) return CLASP_OK;
+  if (c.dtype != CLASP_FP32 || (c.flags & CLASP_FLAG_MULTI_KERNEL) || is_kv4(c)) return CLASP_OK;
   const int d = c.d_model, qd = c.n_q_heads * c.head_dim, kvd = c.n_kv_heads * c.head_dim, cap = s32::MAX_F * s32::WARPS;
   if (c.L > s32::MAX_L || c.max_M + 1 > s32::MAX_STATES || s32::slice_cap(qd + 2 * kvd) > cap || s32::slice_cap(d) > cap ||
       2 * s32::slice_cap(c.d_ffn) > cap)
@@ -802,7 +911,7 @@ namespace pk = clasp::pk;
 int engine_setup(clasp_ctx* ctx) {
   const clasp_config& c = ctx->cfg;
   ctx->use_engine = false;
-  if (!ctx->use_tc || (c.flags & CLASP_FLAG_MULTI_KERNEL)) return CLASP_OK;
+  if (!ctx->use_tc || (c.flags & CLASP_FLAG_MULTI_KERNEL) || is_kv4(c)) return CLASP_OK;
   int dev = 0, coop = 0, optin = 0;
   CUDA_TRY(cudaGetDevice(&dev));
   CUDA_TRY(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
@@ -1258,6 +1367,7 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
   ctx->layers.resize(cfg->L);
   ctx->loaded.assign(cfg->L, 0);
   ctx->num_sms = prop.multiProcessorCount;
+  ctx->device = dev;
   ctx->use_tc = cfg->dtype == CLASP_BF16 && !(cfg->flags & CLASP_FLAG_FORCE_SIMT);
   if (ctx->use_tc) {
     if (prop.major != 10) {  // the tcgen05 kernel exists for sm_100a only
@@ -1284,7 +1394,8 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
     ctx->cta_cap = 2 * ctx->num_sms;
   }
   if (cudaMemsetAsync(ws.status, 0, 256, ctx->stream) != cudaSuccess ||
-      cudaMemsetAsync(ws.counters, 0, MAX_COUNTERS * sizeof(int), ctx->stream) != cudaSuccess) {
+      cudaMemsetAsync(ws.counters, 0, MAX_COUNTERS * sizeof(int), ctx->stream) != cudaSuccess ||
+      (is_kv4(*cfg) && cudaMemsetAsync(ws.kv4_counters, 0, ws.kv4_counter_bytes, ctx->stream) != cudaSuccess)) {
     delete ctx;
     return CLASP_ERR_CUDA;
   }
@@ -1293,8 +1404,9 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
     return CLASP_ERR_CUDA;
   }
   if (ctx->use_tc) {
-    if (engine_setup(ctx) != CLASP_OK || cudaMemsetAsync(ws.ctl, 0, 256, ctx->stream) != cudaSuccess ||
-        cudaMemsetAsync(ws.e_att_acc, 0, ws.e_att_bytes, ctx->stream) != cudaSuccess) {
+    if (engine_setup(ctx) != CLASP_OK ||
+        (!is_kv4(*cfg) && (cudaMemsetAsync(ws.ctl, 0, 256, ctx->stream) != cudaSuccess ||
+                           cudaMemsetAsync(ws.e_att_acc, 0, ws.e_att_bytes, ctx->stream) != cudaSuccess))) {
       delete ctx;
       return CLASP_ERR_CUDA;
     }
@@ -1729,6 +1841,89 @@ int clasp_accept(const int32_t* draft, const int32_t* full_argmax, int32_t K, in
   committed[a] = full_argmax[a];
   *n_accepted = a;
   return CLASP_OK;
+}
+
+size_t clasp_kv4_bytes(const clasp_config* cfg) {
+  if (!config_ok(cfg) || !is_kv4(*cfg)) return 0;
+  return clasp::kv4::array_bytes(cfg->n_kv_heads, cfg->head_dim, cfg->max_ctx);
+}
+
+static int kv4_check(const clasp_ctx* ctx, const clasp_kv_layer* kv) {
+  if (!ctx || !kv || !kv->k || !kv->v || !is_kv4(ctx->cfg) || !kv_aligned(kv, 1)) return CLASP_ERR_INVALID_ARG;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return CLASP_ERR_CUDA;
+  return dev == ctx->device ? CLASP_OK : CLASP_ERR_INVALID_ARG;
+}
+// rows of `heads` heads in the model dtype: 16-byte aligned, at least a row apart
+static bool kv4_rows_ok(const clasp_ctx* ctx, const void* p, int64_t stride, int heads) {
+  return p && al16(p) && stride >= (int64_t)heads * ctx->cfg.head_dim && stride % (ctx->cfg.dtype == CLASP_BF16 ? 8 : 4) == 0;
+}
+
+int clasp_kv4_write(clasp_ctx* ctx, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n, int32_t pos0,
+                    const clasp_kv_layer* kv) {
+  int rc = kv4_check(ctx, kv);
+  if (rc) return rc;
+  const clasp_config& c = ctx->cfg;
+  if (n < 0 || pos0 < 0) return CLASP_ERR_INVALID_ARG;
+  if ((int64_t)pos0 + n > c.max_ctx) return CLASP_ERR_CAPACITY;
+  if (n == 0) return CLASP_OK;
+  if (!kv4_rows_ok(ctx, k, k_stride, c.n_kv_heads) || !kv4_rows_ok(ctx, v, v_stride, c.n_kv_heads)) return CLASP_ERR_INVALID_ARG;
+  const long long units = (long long)n * c.n_kv_heads * (c.head_dim / clasp::kv4::BLOCK);
+  const dim3 grid((unsigned)((units + 255) / 256), 2);
+  const auto ck = kv4_view(ctx, kv->k, c.max_ctx), cv = kv4_view(ctx, kv->v, c.max_ctx);
+  if (c.dtype == CLASP_BF16)
+    clasp::kv4::write_kernel<bf16><<<grid, 256, 0, ctx->stream>>>((const bf16*)k, k_stride, (const bf16*)v, v_stride, n, pos0,
+                                                                 c.n_kv_heads, c.head_dim, ck, cv);
+  else
+    clasp::kv4::write_kernel<float><<<grid, 256, 0, ctx->stream>>>((const float*)k, k_stride, (const float*)v, v_stride, n, pos0,
+                                                                  c.n_kv_heads, c.head_dim, ck, cv);
+  return launch_check(ctx);
+}
+
+int clasp_kv4_read(clasp_ctx* ctx, const clasp_kv_layer* kv, int32_t pos0, int32_t n, void* k_out, int64_t k_stride, void* v_out,
+                   int64_t v_stride) {
+  int rc = kv4_check(ctx, kv);
+  if (rc) return rc;
+  const clasp_config& c = ctx->cfg;
+  if (n < 0 || pos0 < 0) return CLASP_ERR_INVALID_ARG;
+  if ((int64_t)pos0 + n > c.max_ctx) return CLASP_ERR_CAPACITY;
+  if (n == 0) return CLASP_OK;
+  if (!kv4_rows_ok(ctx, k_out, k_stride, c.n_kv_heads) || !kv4_rows_ok(ctx, v_out, v_stride, c.n_kv_heads)) return CLASP_ERR_INVALID_ARG;
+  const long long units = (long long)n * c.n_kv_heads * (c.head_dim / clasp::kv4::BLOCK);
+  const dim3 grid((unsigned)((units + 255) / 256), 2);
+  const auto ck = kv4_view(ctx, kv->k, c.max_ctx), cv = kv4_view(ctx, kv->v, c.max_ctx);
+  if (c.dtype == CLASP_BF16)
+    clasp::kv4::read_kernel<bf16><<<grid, 256, 0, ctx->stream>>>(ck, cv, n, pos0, c.n_kv_heads, c.head_dim, (bf16*)k_out, k_stride,
+                                                                (bf16*)v_out, v_stride);
+  else
+    clasp::kv4::read_kernel<float><<<grid, 256, 0, ctx->stream>>>(ck, cv, n, pos0, c.n_kv_heads, c.head_dim, (float*)k_out, k_stride,
+                                                                 (float*)v_out, v_stride);
+  return launch_check(ctx);
+}
+
+int clasp_kv4_attention(clasp_ctx* ctx, const void* q, int64_t q_stride, int32_t S, int32_t T, int32_t ctx_len, int32_t own_pos0,
+                        const int32_t* visible, const clasp_kv_layer* kv, void* out, int64_t out_stride) {
+  int rc = kv4_check(ctx, kv);
+  if (rc) return rc;
+  const clasp_config& c = ctx->cfg;
+  if (S < 0 || T < 0 || ctx_len < 0 || own_pos0 < -1 || ((uintptr_t)visible & 3)) return CLASP_ERR_INVALID_ARG;
+  const int64_t R = (int64_t)S * T;
+  if (R > c.max_rows || ctx_len > c.max_ctx || (own_pos0 >= 0 && own_pos0 + R > c.max_ctx)) return CLASP_ERR_CAPACITY;
+  if (R == 0) return CLASP_OK;
+  if (!kv4_rows_ok(ctx, q, q_stride, c.n_q_heads) || !kv4_rows_ok(ctx, out, out_stride, c.n_q_heads)) return CLASP_ERR_INVALID_ARG;
+  clasp::kv4::AttnArgs p{};
+  p.q = q; p.q_stride = q_stride; p.q_bf16 = c.dtype == CLASP_BF16;
+  p.out = out; p.out_stride = out_stride; p.out_bf16 = c.dtype == CLASP_BF16;
+  p.R_all = (int)R; p.T = T; p.n_keys = ctx_len; p.visible = visible;
+  p.k = p.own_k = kv4_view(ctx, kv->k, c.max_ctx);
+  p.v = p.own_v = kv4_view(ctx, kv->v, c.max_ctx);
+  if (own_pos0 >= 0) {
+    p.own_pos0 = own_pos0;
+    p.own_n = (int)R;
+    // rows right behind the context they see: one prefix per row
+    if (S == 1 && own_pos0 == ctx_len && !visible) { p.causal = 1; p.n_keys = ctx_len + T; p.own_n = 0; }
+  }
+  return kv4_attend(ctx, p);
 }
 
 int clasp_gemm_xwT(clasp_ctx* ctx, const void* x, const void* w, int32_t R, int32_t N, int32_t K, float* y) {

@@ -1,0 +1,686 @@
+// Key/value cache held in 4 bits (CLASP_FLAG_KV4): rows quantised into it, rows read back, attention over it.
+//
+// A block is 16 consecutive dims of one (position, kv head) row of K or V:
+//   value = (c - 8) * s        c: 4 bits, 1..15;   s: one byte b, the half-precision number with the bits b << 7
+// s is the smallest such number with 7 s >= max |x| (at most 896, then |x| > 6272 saturates), c - 8 = x / s to the
+// nearest, ties to even.  Every step of that is exact in fp32 (7 s has 7 significant bits, a border (k + 1/2) s has 8, a
+// correctly rounded quotient never reaches a border that x / s does not), so the bytes are a function of the row alone.  A
+// value has at most 8 significant bits: exact in bf16 and in half precision.  Sixteen dims per scale: uniform steps of
+// 2/15 of a block's range leave a Gaussian row 7.7 % of its standard deviation as error (4-bit floating point with the same
+// scale byte 9.6 %).  A block that holds an infinity or NaN gets the byte 0xFF and reads back as NaN throughout.
+//
+// One layer's array (keys or values): codes [n_kv, capacity, hd / 2], low nibble first, then scale bytes
+// [n_kv, capacity, hd / 16].  Head-major: what one CTA of the attention reads is contiguous.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace clasp {
+namespace kv4 {
+
+using bf16 = __nv_bfloat16;
+constexpr int BLOCK = 16;
+constexpr uint32_t TOP_SCALE = 0xC6;   // 896: 72 s, which the code-to-half conversion needs, stays finite
+constexpr uint32_t NAN_SCALE = 0xFF;
+
+// One layer's array as the kernels see it.
+struct View {
+  uint8_t* codes;
+  uint8_t* scales;
+  long long head_codes;    // bytes from one kv head to the next
+  long long head_scales;
+};
+inline View view(void* p, int n_kv, int hd, long long capacity) {
+  View v;
+  v.codes = (uint8_t*)p;
+  v.head_codes = capacity * (hd / 2);
+  v.head_scales = capacity * (hd / BLOCK);
+  v.scales = v.codes + v.head_codes * n_kv;
+  return v;
+}
+inline size_t array_bytes(int n_kv, int hd, long long capacity) {
+  return (size_t)n_kv * (size_t)capacity * (size_t)(hd / 2 + hd / BLOCK);
+}
+
+__device__ __forceinline__ float scale_of(uint32_t b) { return __half2float(__ushort_as_half((unsigned short)(b << 7))); }
+
+// Sixteen values -> eight bytes of codes and the scale byte.
+__device__ __forceinline__ uint2 quantise(const float (&x)[BLOCK], uint32_t& byte) {
+  float a = 0.f, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < BLOCK; ++i) {
+    a = fmaxf(a, fabsf(x[i]));
+    sum += fabsf(x[i]) * 0.f;          // NaN exactly when some value is not finite
+  }
+  if (sum != 0.f) {
+    byte = NAN_SCALE;
+    return make_uint2(0x88888888u, 0x88888888u);
+  }
+  // candidate: a / 7 cut to three mantissa bits (the product errs by less than one step of them); the next one if that is
+  // too small.  a below 2^-17: the smallest scale.
+  const float t = fminf(a * (1.0f / 7.0f), 896.f);
+  const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rz(t)) >> 7;
+  byte = min(h + (7.f * scale_of(h) < a ? 1u : 0u), TOP_SCALE);
+  const float s = scale_of(byte);
+  const float r = byte ? __frcp_rn(s) : 0.f;
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < BLOCK; ++i) {
+    // x / s, correctly rounded: reciprocal to the nearest, then one residual step (Markstein's division)
+    const float q0 = x[i] * r;
+    const float q = fmaf(fmaf(-q0, s, x[i]), r, q0);
+    const float c = fminf(fmaxf(rintf(q), -7.f), 7.f) + 8.f;
+    w[i >> 3] |= (uint32_t)c << ((i & 7) * 4);
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ void load16(const float* p, float (&x)[BLOCK]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = reinterpret_cast<const float4*>(p)[i];
+    x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+  }
+}
+__device__ __forceinline__ void load16(const bf16* p, float (&x)[BLOCK]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[8 * i + 2 * k] = __uint_as_float(u[k] << 16);
+      x[8 * i + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+    }
+  }
+}
+__device__ __forceinline__ void store16(float* p, const float (&x)[BLOCK]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    reinterpret_cast<float4*>(p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void store16(bf16* p, const float (&x)[BLOCK]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<uint4*>(p)[i] = make_uint4(pack_bf16(x[8 * i], x[8 * i + 1]), pack_bf16(x[8 * i + 2], x[8 * i + 3]),
+                                                pack_bf16(x[8 * i + 4], x[8 * i + 5]), pack_bf16(x[8 * i + 6], x[8 * i + 7]));
+}
+
+// ------------------------------------------------------------------ rows into the cache and back
+// A thread takes one block of K or of V (blockIdx.y); consecutive threads take consecutive blocks of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) write_kernel(const T* __restrict__ k, long long k_stride, const T* __restrict__ v,
+                                                    long long v_stride, int n, long long pos0, int n_kv, int hd, View ck, View cv) {
+  const int per_head = hd / BLOCK, per_row = n_kv * per_head;
+  const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (u >= (long long)n * per_row) return;
+  const long long row = u / per_row;
+  const int b = (int)(u - row * per_row), head = b / per_head, j = b - head * per_head;
+  const bool val = blockIdx.y != 0;
+  const View& c = val ? cv : ck;
+  float x[BLOCK];
+  load16((val ? v + row * v_stride : k + row * k_stride) + b * BLOCK, x);
+  uint32_t byte;
+  const uint2 w = quantise(x, byte);
+  *reinterpret_cast<uint2*>(c.codes + head * c.head_codes + (pos0 + row) * (hd / 2) + j * 8) = w;
+  c.scales[head * c.head_scales + (pos0 + row) * per_head + j] = (uint8_t)byte;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) read_kernel(View ck, View cv, int n, long long pos0, int n_kv, int hd, T* __restrict__ k,
+                                                   long long k_stride, T* __restrict__ v, long long v_stride) {
+  const int per_head = hd / BLOCK, per_row = n_kv * per_head;
+  const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (u >= (long long)n * per_row) return;
+  const long long row = u / per_row;
+  const int b = (int)(u - row * per_row), head = b / per_head, j = b - head * per_head;
+  const bool val = blockIdx.y != 0;
+  const View& c = val ? cv : ck;
+  const uint2 w = *reinterpret_cast<const uint2*>(c.codes + head * c.head_codes + (pos0 + row) * (hd / 2) + j * 8);
+  const float s = scale_of(c.scales[head * c.head_scales + (pos0 + row) * per_head + j]);
+  float x[BLOCK];
+#pragma unroll
+  for (int i = 0; i < BLOCK; ++i) x[i] = ((float)(((i < 8 ? w.x : w.y) >> ((i & 7) * 4)) & 15u) - 8.f) * s;
+  store16((val ? v + row * v_stride : k + row * k_stride) + b * BLOCK, x);
+}
+
+// A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated in place, keys rotated and quantised, values
+// quantised.  Dims i and i + hd / 2 share a rotation, so a thread of the rotated part takes the blocks j and j + hd / 32.
+__global__ void __launch_bounds__(256) store_rows_kernel(float* __restrict__ qkv, long long ld, const float2* __restrict__ cs, int R,
+                                                         int T, int nq, int nkv, int hd, View ck, View cv, long long pos0) {
+  const int half_blocks = hd / (2 * BLOCK), per_row = (nq + 2 * nkv) * half_blocks;
+  const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (u >= (long long)R * per_row) return;
+  const int r = (int)(u / per_row), e = (int)(u - (long long)r * per_row), head = e / half_blocks, j = e - head * half_blocks;
+  float* p = qkv + r * ld + head * hd + j * BLOCK;
+  float a[BLOCK], b[BLOCK];
+  load16(p, a);
+  load16(p + hd / 2, b);
+  if (head < nq + nkv) {
+    const float2* w = cs + (long long)(r % T) * (hd / 2) + j * BLOCK;
+#pragma unroll
+    for (int i = 0; i < BLOCK; ++i) {
+      const float2 c = w[i];
+      const float x = a[i] * c.x - b[i] * c.y, y = b[i] * c.x + a[i] * c.y;
+      a[i] = x;
+      b[i] = y;
+    }
+    if (head < nq) {
+      store16(p, a);
+      store16(p + hd / 2, b);
+      return;
+    }
+  }
+  const bool val = head >= nq + nkv;
+  const View& c = val ? cv : ck;
+  const int h = head - nq - (val ? nkv : 0);
+  uint8_t* codes = c.codes + h * c.head_codes + (pos0 + r) * (hd / 2) + j * 8;
+  uint8_t* scales = c.scales + h * c.head_scales + (pos0 + r) * (hd / BLOCK) + j;
+  uint32_t byte;
+  *reinterpret_cast<uint2*>(codes) = quantise(a, byte);
+  scales[0] = (uint8_t)byte;
+  *reinterpret_cast<uint2*>(codes + hd / 4) = quantise(b, byte);
+  scales[half_blocks] = (uint8_t)byte;
+}
+
+// ------------------------------------------------------------------ attention
+// Rows are S states of T rows (row r: state r / T).  Row r sees the cache positions [0, limit_r) and, where the call has
+// own rows, the rows first..r of its state, which lie at own + own_pos0.  When the own rows continue the cache (a
+// verification: one state behind the context), the two are one prefix and own_n is 0: limit_r = prefix + r + 1.
+struct AttnArgs {
+  const void* q;           // row r, head h at q + r * q_stride + h * hd, float or bf16
+  long long q_stride;
+  int q_bf16;
+  void* out;
+  long long out_stride;
+  int out_bf16;
+  int R, T, nq, nkv;
+  View k, v;               // the cache
+  int n_keys;              // positions any row may see
+  int causal;              // 1: limit_r = n_keys - R + r + 1
+  const int* visible;      // or null: limit_r = min(n_keys, max(0, visible[r]))
+  View own_k, own_v;
+  long long own_pos0;
+  int own_n;               // rows of the own region (R_all), or 0
+  int run_len, runs;       // keys per CTA and CTAs over the cache; one more CTA where own_n > 0
+  float* part;             // [R * nq, parts, hd] and
+  float2* part_ml;         // [R * nq, parts] (maximum, sum)
+  int* counters;           // one per (kv head, block of pairs), zero on entry and on exit
+  int r0;                  // first row of this launch (of `visible` and the causal limit; q, out are offset already)
+  int R_all;               // rows of the call
+};
+
+__device__ __forceinline__ int row_limit(const AttnArgs& p, int r) {
+  if (p.causal) return p.n_keys - p.R_all + p.r0 + r + 1;
+  if (p.visible) return min(p.n_keys, max(0, p.visible[p.r0 + r]));
+  return p.n_keys;
+}
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix_t(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
+__device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+// lanes of a 32-bit logic operation: (x & m) | o
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t o) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(m), "r"(o));
+  return y;
+}
+
+// Scales of the two halves of a register, as the conversion needs them.
+struct Scale2 {
+  __half2 s, s16, m72;   // s, s / 16, -72 s
+};
+__device__ __forceinline__ Scale2 scale2(uint32_t b_lo, uint32_t b_hi) {
+  Scale2 r;
+  r.s = as_half2((b_lo << 7) | (b_hi << 23));
+  r.s16 = __hmul2(r.s, as_half2(0x2C002C00u));    // 1 / 16
+  r.m72 = __hmul2(r.s, as_half2(0xD480D480u));    // -72
+  return r;
+}
+// The nibbles 0, 1 (w) or 2, 3 (w >> 8) of both 16-bit halves as values (c - 8) s.  A nibble in the low mantissa bits of
+// 1024 makes 1024 + c, one place higher 1024 + 16 c: no integer conversion.  Exact: c - 8 and its product with s have
+// few bits; 72 s has 7 (9 x a 4-bit mantissa).  (1024 + c) s - 1032 s in one step would overflow from s = 64 on.
+__device__ __forceinline__ uint32_t nib_lo(uint32_t w, const Scale2& s) {
+  return as_u32(__hmul2(__hsub2(as_half2(and_or(w, 0x000F000Fu, 0x64006400u)), as_half2(0x64086408u)), s.s));
+}
+__device__ __forceinline__ uint32_t nib_hi(uint32_t w, const Scale2& s) {
+  return as_u32(__hfma2(as_half2(and_or(w, 0x00F000F0u, 0x64006400u)), s.s16, s.m72));
+}
+
+constexpr int WARPS = 8;
+constexpr int STEP = 16;                 // keys a warp takes at a time
+constexpr int MAX_PARTS = 152;           // runs of one launch and the own rows
+constexpr float P_BITS = 12.f;           // weights are held as 2^12 .. 2^20 x exp2(s - m) in half precision (see below)
+
+template <int HD> struct Raw {           // one warp step: two key rows' and four value rows' pieces per lane
+  uint32_t k[2][HD / 32], v[4][HD / 64];
+  uint32_t ks[2], vs;
+};
+
+// Attention of few (row, query head) pairs: 8 NT pairs of one kv head per CTA, one run of the cache per CTA, its steps of 16
+// keys dealt to eight warps that never wait for one another before the end.
+//
+//   S^T = K q^T     16 keys x 8 pairs: the keys are the M rows of mma.m16n8k16, so few pairs waste little
+//   O^T = V^T P^T   16 dims x 8 pairs
+//
+// Which key an M row is and which dim a k index is, is free as long as both operands agree, so every lane gets its pieces of
+// K and V by 16- and 8-byte loads straight from the cache (no shared memory) and converts them in place: lane (g, t) of a
+// step holds dims [32 t, 32 t + 32) of two keys, and 16 dims [16 g, 16 g + 16) of four values (hd 128).  K and V are exact in
+// half precision.  q is scaled by a power of two per row to a largest magnitude in [2^13, 2^14) and rounded to half precision:
+// exact for bf16 rows (what lies 2^24 below the row's maximum aside); SPLIT (fp32 models) adds the rounding error of q and of
+// the weights as a second half-precision operand: 22 bits.  Weights: half precision of 2^12 exp2(s - m), m a maximum that moves
+// only when exceeded by 2^3, so they stay below 2^15 and lose nothing above 2^-26 of the largest; sums in fp32.
+// A block with the NaN byte must reach only the rows that see it, and 0 x NaN is NaN: values' NaN blocks enter as zeros, and
+// `poison` remembers which (pair, block) they belong to.
+template <int HD, int NT, bool SPLIT>
+__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(const __grid_constant__ AttnArgs p) {
+  constexpr int PB = 8 * NT;             // pairs per CTA
+  constexpr int KS = HD / 16;            // k steps of the scores, and tiles of 16 dims of the output
+  constexpr int KW = HD / 32, VW = HD / 64;
+  constexpr int PARTS = SPLIT ? 2 : 1;
+  constexpr float NEG = -INFINITY;
+  __shared__ uint2 qf[PARTS][NT][KS][32];
+  __shared__ float o_sm[WARPS][8][HD + 4];
+  __shared__ float2 ml_sm[WARPS][PB];
+  __shared__ float mult_sm[PB];
+  __shared__ int lo_sm[PB], hi_sm[PB];
+  __shared__ uint32_t poison_sm[8];
+  __shared__ int range_sm[4];            // largest lo, smallest hi, smallest lo, largest hi
+  __shared__ int last_sm;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int run = blockIdx.x, kvh = blockIdx.y, pb = blockIdx.z;
+  const int G = p.nq / p.nkv, n_pairs = p.R * G, parts = gridDim.x;
+  const bool own = run >= p.runs;
+  const int pair0 = pb * PB;
+
+  if (threadIdx.x < 8) poison_sm[threadIdx.x] = 0;
+  if (threadIdx.x == 8) { range_sm[0] = 0; range_sm[1] = 0x7fffffff; range_sm[2] = 0x7fffffff; range_sm[3] = 0; }
+  __syncthreads();
+  if (threadIdx.x < PB) {
+    const int pp = pair0 + (int)threadIdx.x;
+    int lo = 0, hi = 0;
+    if (pp < n_pairs) {
+      const int r = pp / G;
+      if (own) { lo = (p.r0 + r) / p.T * p.T; hi = p.r0 + r + 1; }
+      else hi = row_limit(p, r);
+      atomicMax(&range_sm[0], lo);
+      atomicMin(&range_sm[1], hi);
+      atomicMin(&range_sm[2], lo);
+      atomicMax(&range_sm[3], hi);
+    }
+    lo_sm[threadIdx.x] = lo;
+    hi_sm[threadIdx.x] = hi;
+  }
+  // q rows into the fragments of the second operand: a warp per pair, lane = its place along the row
+  for (int i = warp; i < PB; i += WARPS) {
+    const int pp = pair0 + i;
+    constexpr int E = HD / 32;
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.f;
+    if (pp < n_pairs) {
+      const long long off = (long long)(pp / G) * p.q_stride + (long long)(kvh * G + pp % G) * HD + lane * E;
+      if (p.q_bf16) {
+        const bf16* s = (const bf16*)p.q + off;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = __bfloat162float(s[e]);
+      } else {
+        const float* s = (const float*)p.q + off;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = s[e];
+      }
+    }
+    float a = 0.f, bad = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) { a = fmaxf(a, fabsf(x[e])); bad += x[e] * 0.f; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+      bad += __shfl_xor_sync(0xffffffffu, bad, o);
+    }
+    // power of two that brings the largest magnitude into [2^13, 2^14); rows far below 2^-113 are as good as zero
+    const int ex = max((int)(__float_as_uint(a) >> 23) - 127, -113);
+    const float up1 = __uint_as_float((uint32_t)(127 + ((13 - ex) >> 1)) << 23);
+    const float up2 = __uint_as_float((uint32_t)(127 + (13 - ex) - ((13 - ex) >> 1)) << 23);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = x[e] * up1 * up2;
+    // element d of the row is half h of register b of lane (g = i & 7, t = d / (HD / 4)) in step 2 (word) + (n & 3) / 2, for
+    // word = d % (HD / 4) / 8, n = d % 8: b = n & 1, half n / 4
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int d = lane * E + e, tt = d / (HD / 4), wd = d % (HD / 4) / 8, n = d & 7;
+      const int step = wd * 2 + ((n >> 1) & 1);
+      const __half hx = __float2half_rn(x[e]);
+      __half* dst = reinterpret_cast<__half*>(&qf[0][i >> 3][step][(i & 7) * 4 + tt]) + (n & 1) * 2 + (n >> 2);
+      *dst = hx;
+      if constexpr (SPLIT) {
+        __half* d2 = reinterpret_cast<__half*>(&qf[PARTS - 1][i >> 3][step][(i & 7) * 4 + tt]) + (n & 1) * 2 + (n >> 2);
+        *d2 = __float2half_rn(x[e] - __half2float(hx));
+      }
+    }
+    if (lane == 0) {
+      // scores in units of log2: q.k / sqrt(hd) log2(e), the row's power of two taken back.  A row with an infinity or NaN in
+      // it has no finite score: all its weights are NaN.
+      const float c = 1.4426950408889634f * rsqrtf((float)HD);
+      const float dn1 = __uint_as_float((uint32_t)(127 - ((13 - ex) >> 1)) << 23);
+      const float dn2 = __uint_as_float((uint32_t)(127 - ((13 - ex) - ((13 - ex) >> 1))) << 23);
+      mult_sm[i] = bad == 0.f ? c * dn1 * dn2 : __int_as_float(0x7fffffff);
+    }
+  }
+  __syncthreads();
+
+  // keys of this CTA
+  int k_lo, k_end;
+  if (own) {
+    k_lo = range_sm[2];
+    k_end = min(range_sm[3], p.own_n);
+  } else {
+    k_lo = run * p.run_len;
+    k_end = min(min(k_lo + p.run_len, p.n_keys), range_sm[3]);
+  }
+  const int full_lo = range_sm[0], full_hi = min(range_sm[1], k_end);
+  const long long pos_off = own ? p.own_pos0 : 0;
+  const View& vk = own ? p.own_k : p.k;
+  const View& vv = own ? p.own_v : p.v;
+  const uint8_t* kc = vk.codes + kvh * vk.head_codes + pos_off * (HD / 2) + t * (HD / 8);
+  const uint8_t* kx = vk.scales + kvh * vk.head_scales + pos_off * (HD / BLOCK) + t * (HD / 64);
+  const uint8_t* vc = vv.codes + kvh * vv.head_codes + pos_off * (HD / 2) + g * (HD / 16);
+  const uint8_t* vx = vv.scales + kvh * vv.head_scales + pos_off * (HD / BLOCK) + (HD == 128 ? g : g >> 1);
+  const int kg = (g >> 1) + 4 * (g & 1);   // key of M row g; row g + 8 is key kg + 8
+
+  auto fetch = [&](Raw<HD>& w, int base) {
+    const int top = k_end - 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const long long key = min(base + kg + 8 * i, top);
+      if constexpr (HD == 128) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(kc + key * 64));
+        w.k[i][0] = u.x; w.k[i][1] = u.y; w.k[i][2] = u.z; w.k[i][3] = u.w;
+        w.ks[i] = __ldg(reinterpret_cast<const unsigned short*>(kx + key * 8));
+      } else {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(kc + key * 32));
+        w.k[i][0] = u.x; w.k[i][1] = u.y;
+        w.ks[i] = __ldg(kx + key * 4);
+      }
+    }
+    w.vs = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long key = min(base + t + 4 * i, top);
+      if constexpr (HD == 128) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(vc + key * 64));
+        w.v[i][0] = u.x; w.v[i][1] = u.y;
+        w.vs |= (uint32_t)__ldg(vx + key * 8) << (8 * i);
+      } else {
+        w.v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(vc + key * 32));
+        w.vs |= (uint32_t)__ldg(vx + key * 4) << (8 * i);
+      }
+    }
+  };
+
+  float o[NT][KS][4], m[NT][2], l[NT][2], mult[NT][2];
+  uint32_t poison = 0;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) { m[n][c] = NEG; l[n][c] = 0.f; mult[n][c] = mult_sm[n * 8 + 2 * t + c]; }
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[n][j][c] = 0.f;
+  }
+
+  int base = k_lo + warp * STEP;
+  Raw<HD> cur, nxt;
+  if (base < k_end) fetch(cur, base);
+  for (; base < k_end; base += WARPS * STEP) {
+    const bool more = base + WARPS * STEP < k_end;
+    if (more) fetch(nxt, base + WARPS * STEP);
+    // ---- scores
+    float s[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[n][c] = 0.f;
+#pragma unroll
+    for (int wd = 0; wd < KW; ++wd) {
+      const int sh = HD == 128 ? (wd >> 1) * 8 : 0;   // two words per scale
+      const uint32_t b0 = (cur.ks[0] >> sh) & 255u, b1 = (cur.ks[1] >> sh) & 255u;
+      const Scale2 s0 = scale2(b0, b0), s1 = scale2(b1, b1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t w0 = cur.k[0][wd] >> (8 * h), w1 = cur.k[1][wd] >> (8 * h);
+        const uint32_t a[4] = {nib_lo(w0, s0), nib_lo(w1, s1), nib_hi(w0, s0), nib_hi(w1, s1)};
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) {
+            const uint2 b = qf[q][n][wd * 2 + h][lane];
+            mma16816(s[n], a, b.x, b.y);
+          }
+      }
+    }
+    // ---- masks, weights
+    const bool full = base >= full_lo && base + STEP <= full_hi;
+    uint32_t pw[PARTS][NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[n][c] *= mult[n][c & 1];
+      if (!full) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int key = base + kg + (c >> 1) * 8, col = n * 8 + 2 * t + (c & 1);
+          if (key < lo_sm[col] || key >= min(hi_sm[col], k_end)) s[n][c] = NEG;
+        }
+      }
+      const float x0 = fmaxf(s[n][0], s[n][2]), x1 = fmaxf(s[n][1], s[n][3]);
+      if (__any_sync(0xffffffffu, x0 > m[n][0] + 3.f || x1 > m[n][1] + 3.f)) {
+        float y[2] = {x0, x1};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) y[c] = fmaxf(y[c], __shfl_xor_sync(0xffffffffu, y[c], d));
+          if (y[c] > m[n][c] + 3.f) {
+            const float corr = exp2f(m[n][c] - y[c]);
+            m[n][c] = y[c];
+            l[n][c] *= corr;
+#pragma unroll
+            for (int j = 0; j < KS; ++j) { o[n][j][c] *= corr; o[n][j][c + 2] *= corr; }
+          }
+        }
+      }
+      float e[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float mm = m[n][c & 1] == NEG ? 0.f : m[n][c & 1] - P_BITS;   // no visible key so far: exp2(-inf) = 0
+        e[c] = ex2(s[n][c] - mm);
+      }
+      l[n][0] += e[0] + e[2];
+      l[n][1] += e[1] + e[3];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t u = pack_half(e[2 * h], e[2 * h + 1]);
+        pw[0][n][h] = movmatrix_t(u);
+        if constexpr (SPLIT) {
+          const float2 f = unpack_half(u);
+          pw[PARTS - 1][n][h] = movmatrix_t(pack_half(e[2 * h] - f.x, e[2 * h + 1] - f.y));
+        }
+      }
+    }
+    // ---- values.  Lane (g, t): keys t, t + 4 are the M-operand's columns 2 t, 2 t + 1, keys t + 8, t + 12 the upper ones
+    if (__vcmpeq4(cur.vs, 0xffffffffu)) {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i)
+        if (((cur.vs >> (8 * i)) & 255u) == NAN_SCALE) {
+          const int key = base + t + 4 * i;
+#pragma unroll 1
+          for (int c = 0; c < PB; ++c)
+            if (key >= lo_sm[c] && key < min(hi_sm[c], k_end)) poison |= 1u << c;
+          cur.vs &= ~(255u << (8 * i));
+        }
+    }
+    const Scale2 z0 = scale2(cur.vs & 255u, (cur.vs >> 8) & 255u), z1 = scale2((cur.vs >> 16) & 255u, cur.vs >> 24);
+#pragma unroll
+    for (int wd = 0; wd < VW; ++wd) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // dims 4 h .. 4 h + 3 of the word, one key in each half
+        const uint32_t x = __byte_perm(cur.v[0][wd], cur.v[1][wd], h ? 0x7632 : 0x5410);
+        const uint32_t y = __byte_perm(cur.v[2][wd], cur.v[3][wd], h ? 0x7632 : 0x5410);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t a[4] = {nib_lo(x >> (8 * e), z0), nib_hi(x >> (8 * e), z0), nib_lo(y >> (8 * e), z1), nib_hi(y >> (8 * e), z1)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) mma16816(o[n][wd * 4 + h * 2 + e], a, pw[q][n][0], pw[q][n][1]);
+        }
+      }
+    }
+    if (more) cur = nxt;
+  }
+
+  // ---- the warps' results together, in warp order
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
+      if (g == 0) ml_sm[warp][n * 8 + 2 * t + c] = make_float2(m[n][c], l[n][c]);
+    }
+  if (poison) atomicOr(&poison_sm[g], poison);
+  __syncthreads();
+  const bool single = parts == 1;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    if (n > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = 2 * t + c;
+      float mx = NEG;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, ml_sm[w][n * 8 + col].x);
+      const float corr = m[n][c] == NEG ? 0.f : exp2f(m[n][c] - mx);
+      const bool bad = (poison_sm[g] >> (n * 8 + col)) & 1u;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        float2 v = make_float2(o[n][j][c] * corr, o[n][j][c + 2] * corr);
+        if (m[n][c] == NEG && l[n][c] == 0.f) v = make_float2(0.f, 0.f);
+        if (bad) v = make_float2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
+        *reinterpret_cast<float2*>(&o_sm[warp][col][g * (HD / 8) + 2 * j]) = v;
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 8 * (HD / 4); i += WARPS * 32) {
+      const int col = i / (HD / 4), d = i % (HD / 4) * 4, pp = pair0 + n * 8 + col;
+      if (pp >= n_pairs) continue;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      float mx = NEG, den = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, ml_sm[w][n * 8 + col].x);
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float4 v = *reinterpret_cast<const float4*>(&o_sm[w][col][d]);
+        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+        const float2 ml = ml_sm[w][n * 8 + col];
+        den += ml.x == NEG ? ml.y : ml.y * exp2f(ml.x - mx);   // (a sum without a maximum is 0, or NaN)
+      }
+      const long long rh = (long long)(pp / G) * p.nq + kvh * G + pp % G;
+      if (single) {
+        const float inv = den == 0.f ? 0.f : 1.0f / den;
+        const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
+        if (p.out_bf16) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+        else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+      } else {
+        *reinterpret_cast<float4*>(p.part + (rh * parts + run) * HD + d) = a;
+        if (d == 0) p.part_ml[rh * parts + run] = make_float2(mx, den);
+      }
+    }
+  }
+  if (single) return;
+
+  // ---- the CTA that arrives last adds the runs, in run order
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int* c = p.counters + (long long)pb * p.nkv + kvh;
+    const int n = atomicAdd(c, 1);
+    last_sm = n == parts - 1;
+    if (n == parts - 1) *c = 0;
+  }
+  __syncthreads();
+  if (!last_sm) return;
+  __threadfence();
+  float* w_sm = &o_sm[0][0][0];          // [8][MAX_PARTS] weights, then [8] 1 / sum
+  static_assert(WARPS * 8 * (HD + 4) >= 8 * MAX_PARTS + 8, "weights fit");
+  for (int n = 0; n < NT; ++n) {
+    __syncthreads();
+    {
+      const int pp = pair0 + n * 8 + warp;   // a warp per pair
+      if (pp < n_pairs) {
+        const float2* ml = p.part_ml + ((long long)(pp / G) * p.nq + kvh * G + pp % G) * parts;
+        float mx = NEG, den = 0.f;
+        for (int i = lane; i < parts; i += 32) mx = fmaxf(mx, __ldcg(&ml[i]).x);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        for (int i = lane; i < parts; i += 32) {
+          const float2 v = __ldcg(&ml[i]);
+          const float w = v.x == NEG ? (v.y == 0.f ? 0.f : 1.f) : exp2f(v.x - mx);
+          w_sm[warp * MAX_PARTS + i] = w;
+          den += v.y * w;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) den += __shfl_xor_sync(0xffffffffu, den, d);
+        if (lane == 0) w_sm[8 * MAX_PARTS + warp] = den == 0.f ? 0.f : 1.0f / den;
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 8 * (HD / 4); i += WARPS * 32) {
+      const int col = i / (HD / 4), d = i % (HD / 4) * 4, pp = pair0 + n * 8 + col;
+      if (pp >= n_pairs) continue;
+      const float* src = p.part + ((long long)(pp / G) * p.nq + kvh * G + pp % G) * parts * HD + d;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int r = 0; r < parts; ++r) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + (long long)r * HD));
+        const float w = w_sm[col * MAX_PARTS + r];
+        a.x = fmaf(w, v.x, a.x); a.y = fmaf(w, v.y, a.y); a.z = fmaf(w, v.z, a.z); a.w = fmaf(w, v.w, a.w);
+      }
+      const float inv = w_sm[8 * MAX_PARTS + col];
+      const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
+      if (p.out_bf16) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+      else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    }
+  }
+}
+
+}  // namespace kv4
+}  // namespace clasp
