@@ -41,6 +41,8 @@ constexpr long long S32_MAX_SCORES = 65536;   // rows x query heads x keys
 constexpr int WIDE_MIN_ROWS = 128;   // layers over more rows take the products and the attention of wide.cuh
 constexpr int KV4_MAX_CTX = 1 << 30;   // positions of a 4-bit cache: key numbers and steps past the end stay in 32 bits
 constexpr int KV4_ROWS = 64;           // rows per launch of the attention of few rows: bounds its workspace
+constexpr int KV4_FEW_ROWS = 16;       // rows of a call (bf16) whose sums do not depend on how many share it
+constexpr size_t KV4_MANY_SLOTS = 160 * 256;   // (pair, part) slots of the attention of many rows: about one CTA's pairs per SM
 constexpr int MAX_COUNTERS = 4096;   // tiles of one GEMM launch that may use split-K
 constexpr size_t PARTIAL_FLOATS = (size_t)296 * 2 * 128 * 128 + (1 << 20);
 
@@ -164,7 +166,8 @@ Workspace carve(const clasp_config& c, uint8_t* base) {
   w.rope = (float2*)take(R * (c.head_dim / 2) * sizeof(float2));
   const size_t att_chunks = clasp::ATT_MAX_CACHE_CHUNKS + (R + clasp::ATT_KEYS - 1) / clasp::ATT_KEYS;
   if (is_kv4(c)) {
-    const size_t slots = std::min(R, (size_t)KV4_ROWS) * c.n_q_heads * kv4_max_parts(c);
+    const size_t slots = std::max(std::min(R, (size_t)(c.dtype == CLASP_BF16 && !(c.flags & CLASP_FLAG_FORCE_SIMT) ? KV4_FEW_ROWS : KV4_ROWS)) *
+                                      c.n_q_heads * kv4_max_parts(c), KV4_MANY_SLOTS);
     w.kv4_part = (float*)take(slots * c.head_dim * 4);
     w.kv4_ml = (float2*)take(slots * sizeof(float2));
     w.kv4_counter_bytes = (size_t)(KV4_ROWS * c.n_q_heads / 8 + c.n_kv_heads) * sizeof(int);
@@ -208,6 +211,18 @@ Workspace carve(const clasp_config& c, uint8_t* base) {
   }
   w.bytes = off;
   return w;
+}
+
+cudaError_t kv4_attributes() {
+  namespace k4 = clasp::kv4;
+  const struct { const void* f; int bytes; } k[] = {
+      {(const void*)k4::attn_many_kernel<128, 1>, k4::many_smem<128, 1>()}, {(const void*)k4::attn_many_kernel<128, 2>, k4::many_smem<128, 2>()},
+      {(const void*)k4::attn_many_kernel<64, 1>, k4::many_smem<64, 1>()}, {(const void*)k4::attn_many_kernel<64, 2>, k4::many_smem<64, 2>()}};
+  for (const auto& e : k) {
+    const cudaError_t rc = cudaFuncSetAttribute(e.f, cudaFuncAttributeMaxDynamicSharedMemorySize, e.bytes);
+    if (rc != cudaSuccess) return rc;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -582,6 +597,13 @@ clasp::kv4::View kv4_view(const clasp_ctx* ctx, void* p, int64_t capacity) {
   return clasp::kv4::view(p, ctx->cfg.n_kv_heads, ctx->cfg.head_dim, capacity);
 }
 
+// Which kernel: the tensor-core one (tcgen05) from 17 pairs per kv head on -- but verifications and plain calls of up to 16 rows keep the
+// kernel of one-token decoding, so that a row's sums do not depend on the rows that share the call.  fp32 models stay there.
+bool kv4_takes_many(const clasp_config& c, const clasp::kv4::AttnArgs& p) {
+  if (c.dtype != CLASP_BF16 || (c.flags & CLASP_FLAG_FORCE_SIMT)) return false;
+  return p.own_n > 0 ? p.R_all * (c.n_q_heads / c.n_kv_heads) > 16 : p.R_all > KV4_FEW_ROWS;
+}
+
 template <int HD, bool SPLIT>
 int kv4_rows_launch(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
   namespace k4 = clasp::kv4;
@@ -593,6 +615,22 @@ int kv4_rows_launch(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
   if (nt == 1) k4::attn_rows_kernel<HD, 1, SPLIT><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
   else if (nt == 2) k4::attn_rows_kernel<HD, 2, SPLIT><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
   else if constexpr (!SPLIT) k4::attn_rows_kernel<HD, 4, false><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
+  return launch_check(ctx);
+}
+
+template <int HD, int NB>
+int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
+  namespace k4 = clasp::kv4;
+  const int pairs = p.R * (p.nq / p.nkv);
+  p.blocks = (pairs + NB * k4::TP - 1) / (NB * k4::TP);
+  // few blocks: their key tiles are split so that every SM has work
+  const int items = p.blocks * p.nkv, keys = p.n_keys + (p.own_n > 0 ? std::min(p.own_n, NB * k4::TP + p.T) : 0);
+  p.splits = std::max(1, std::min(ctx->num_sms / items, (keys + k4::TK - 1) / k4::TK));
+  if ((size_t)p.splits > 1 && (size_t)p.R * p.nq * p.splits > KV4_MANY_SLOTS) p.splits = 1;
+  k4::attn_many_kernel<HD, NB><<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
+  int rc = launch_check(ctx);
+  if (rc || p.splits == 1) return rc;
+  k4::merge_kernel<HD><<<(unsigned)(((long long)p.R * p.nq + 7) / 8), 256, 0, ctx->stream>>>(p);
   return launch_check(ctx);
 }
 
@@ -609,6 +647,16 @@ int kv4_attend(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
   const void* q = p.q;
   void* out = p.out;
   const bool split = c.dtype == CLASP_FP32;
+  if (kv4_takes_many(c, p)) {
+    p.R = p.R_all;
+    p.r0 = 0;
+    p.status = ctx->ws.status;
+    p.spin_fast = ctx->wait_limit ? std::min(ctx->wait_limit, clasp::tc::SPIN_FAST) : clasp::tc::SPIN_FAST;
+    p.spin_slow = ctx->wait_limit ? ctx->wait_limit : clasp::tc::SPIN_SLOW;
+    const bool one = p.R * (p.nq / p.nkv) <= clasp::kv4::TP;
+    if (c.head_dim == 128) return one ? kv4_many_launch<128, 1>(ctx, p) : kv4_many_launch<128, 2>(ctx, p);
+    return one ? kv4_many_launch<64, 1>(ctx, p) : kv4_many_launch<64, 2>(ctx, p);
+  }
   for (int r0 = 0; r0 < p.R_all; r0 += KV4_ROWS) {
     p.r0 = r0;
     p.R = std::min(KV4_ROWS, p.R_all - r0);
@@ -1387,7 +1435,8 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
         cudaFuncSetAttribute(clasp::wide::gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, clasp::wide::GEMM_SMEM) !=
             cudaSuccess ||
         cudaFuncSetAttribute(clasp::wide::attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, clasp::wide::ATT_SMEM) !=
-            cudaSuccess) {
+            cudaSuccess ||
+        kv4_attributes() != cudaSuccess) {
       delete ctx;
       return CLASP_ERR_CUDA;
     }

@@ -17,6 +17,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "gemm_tc.cuh"
+#include "wide.cuh"
+
 namespace clasp {
 namespace kv4 {
 
@@ -212,6 +215,9 @@ struct AttnArgs {
   float* part;             // [R * nq, parts, hd] and
   float2* part_ml;         // [R * nq, parts] (maximum, sum)
   int* counters;           // one per (kv head, block of pairs), zero on entry and on exit
+  int* status;             // set when a bounded wait of attn_many_kernel runs out
+  uint32_t spin_fast, spin_slow;
+  int blocks, splits;      // attn_many_kernel: blocks of pairs per kv head, parts of each block's key tiles
   int r0;                  // first row of this launch (of `visible` and the causal limit; q, out are offset already)
   int R_all;               // rows of the call
 };
@@ -250,6 +256,32 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t o) {
   uint32_t y;
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(m), "r"(o));
   return y;
+}
+
+// A query row for half precision: the power of two (in two factors) that brings its largest magnitude into [2^13, 2^14), and
+// the factor that takes it back and brings the scores into units of log2 (1 / sqrt(hd) aside).  LANES neighbouring lanes hold a row,
+// N values each.  A row with an infinity or NaN in it has no finite score: its factor is NaN, and so are all its weights.
+struct RowScale {
+  float up1, up2, mult;
+};
+template <int N, int LANES>
+__device__ __forceinline__ RowScale row_scale(const float (&x)[N]) {
+  float a = 0.f, bad = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) { a = fmaxf(a, fabsf(x[e])); bad += x[e] * 0.f; }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+    bad += __shfl_xor_sync(0xffffffffu, bad, o);
+  }
+  const int up = 13 - max((int)(__float_as_uint(a) >> 23) - 127, -113);   // rows far below 2^-113 are as good as zero
+  const int u1 = up >> 1, u2 = up - u1;
+  RowScale r;
+  r.up1 = __uint_as_float((uint32_t)(127 + u1) << 23);
+  r.up2 = __uint_as_float((uint32_t)(127 + u2) << 23);
+  r.mult = 1.4426950408889634f * __uint_as_float((uint32_t)(127 - u1) << 23) * __uint_as_float((uint32_t)(127 - u2) << 23);
+  if (bad != 0.f) r.mult = __int_as_float(0x7fffffff);
+  return r;
 }
 
 // Scales of the two halves of a register, as the conversion needs them.
@@ -356,20 +388,9 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
         for (int e = 0; e < E; ++e) x[e] = s[e];
       }
     }
-    float a = 0.f, bad = 0.f;
+    const RowScale rs = row_scale<E, 32>(x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) { a = fmaxf(a, fabsf(x[e])); bad += x[e] * 0.f; }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-      bad += __shfl_xor_sync(0xffffffffu, bad, o);
-    }
-    // power of two that brings the largest magnitude into [2^13, 2^14); rows far below 2^-113 are as good as zero
-    const int ex = max((int)(__float_as_uint(a) >> 23) - 127, -113);
-    const float up1 = __uint_as_float((uint32_t)(127 + ((13 - ex) >> 1)) << 23);
-    const float up2 = __uint_as_float((uint32_t)(127 + (13 - ex) - ((13 - ex) >> 1)) << 23);
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = x[e] * up1 * up2;
+    for (int e = 0; e < E; ++e) x[e] = x[e] * rs.up1 * rs.up2;
     // element d of the row is half h of register b of lane (g = i & 7, t = d / (HD / 4)) in step 2 (word) + (n & 3) / 2, for
     // word = d % (HD / 4) / 8, n = d % 8: b = n & 1, half n / 4
 #pragma unroll
@@ -384,14 +405,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
         *d2 = __float2half_rn(x[e] - __half2float(hx));
       }
     }
-    if (lane == 0) {
-      // scores in units of log2: q.k / sqrt(hd) log2(e), the row's power of two taken back.  A row with an infinity or NaN in
-      // it has no finite score: all its weights are NaN.
-      const float c = 1.4426950408889634f * rsqrtf((float)HD);
-      const float dn1 = __uint_as_float((uint32_t)(127 - ((13 - ex) >> 1)) << 23);
-      const float dn2 = __uint_as_float((uint32_t)(127 - ((13 - ex) - ((13 - ex) >> 1))) << 23);
-      mult_sm[i] = bad == 0.f ? c * dn1 * dn2 : __int_as_float(0x7fffffff);
-    }
+    if (lane == 0) mult_sm[i] = rs.mult * rsqrtf((float)HD);
   }
   __syncthreads();
 
@@ -680,6 +694,431 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
       else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
     }
   }
+}
+
+// ------------------------------------------------------------------ attention of many pairs
+constexpr int TK = 64;                 // keys per tile
+constexpr int TP = 128;                // pairs per block: tensor-memory lanes
+constexpr int RING = 6;                // K and V tiles, converted, in shared memory
+constexpr float LAZY = 5.f, MANY_BITS = 10.f;   // the maximum moves when exceeded by 2^5; weights are 2^10 exp2(s - m)
+
+template <int HD, int NB>
+constexpr int many_smem() { return NB * TP * HD * 2 + RING * TK * HD * 2 + 2048; }
+template <int NB>
+constexpr int many_threads() { return NB * 128 + 128 + 32; }
+
+struct ManyShared {
+  uint64_t full[RING], empty[RING], s_full[2][2], p_full[2][2];
+  uint64_t o_done[2][2];   // by parity of the tile: a wait that skips tiles may lag one behind, never two
+  float mult[2 * TP];      // per pair: score = product x mult (log2 units)
+  uint32_t tmem_base;
+  int abort, poison, max_hi;
+};
+static_assert(sizeof(ManyShared) <= 2048, "fits its share of shared memory");
+
+// sixteen dims of a row as half-precision values in the order of the codes' conversion: dims 0 4 1 5 2 6 3 7 of each eight
+__device__ __forceinline__ uint4 halves8(const float* x) {
+  return make_uint4(pack_half(x[0], x[4]), pack_half(x[1], x[5]), pack_half(x[2], x[6]), pack_half(x[3], x[7]));
+}
+
+// Attention of many (row, query head) pairs of a kv head: NB blocks of 128 pairs per CTA share the key tiles, which four
+// warps convert from the cache's codes into shared memory (exact half precision, 128-byte swizzle).
+//   S = Q K^T, P = 2^10 exp2(S - m) in half precision, O += P V: tcgen05, S / P / O in tensor memory
+// A thread owns a pair; its maximum moves only when exceeded by 2^5 (then O is rescaled).  Scores are double-buffered: the next
+// tile's Q K^T runs under this tile's softmax.  Scaling of q, NaN blocks: as in attn_rows_kernel; where a value's NaN block was
+// met, the pairs look through the scale bytes of the keys they see once more at the end.
+template <int HD, int NB>
+__global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const __grid_constant__ AttnArgs p) {
+  constexpr int NH = HD / 64;                        // 64-dim halves of a row
+  constexpr uint32_t Q_BYTES = TP * HD * 2, KV_BYTES = TK * HD * 2, HALF_Q = TP * 128, HALF_KV = TK * 128;
+  constexpr uint32_t TM_COLS = NB == 2 ? 512 : 256, O_COL = NB * 128;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t base = tc::smem_u32(smem);
+  ManyShared* sh = reinterpret_cast<ManyShared*>(smem + NB * Q_BYTES + RING * KV_BYTES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int Gq = p.nq / p.nkv, Pn = p.R * Gq;
+  // longest blocks first
+  int b = blockIdx.x;
+  const int split = b % p.splits;
+  b /= p.splits;
+  const int kvh = b % p.nkv;
+  const int pair0 = (p.blocks - 1 - b / p.nkv) * (NB * TP);
+  const int r_lo = pair0 / Gq, r_hi = min(p.R - 1, (pair0 + NB * TP - 1) / Gq);
+  if ((base & 1023u) != 0) {   // the tiles' swizzle needs it (dynamic shared memory starts aligned)
+    if (threadIdx.x == 0) atomicExch(p.status, 1);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < RING; ++s) {
+      tc::mbar_init(tc::smem_u32(&sh->full[s]), 128);
+      tc::mbar_init(tc::smem_u32(&sh->empty[s]), 1);
+    }
+    for (int s = 0; s < 4; ++s) {
+      tc::mbar_init(tc::smem_u32(&sh->s_full[s >> 1][s & 1]), 1);
+      tc::mbar_init(tc::smem_u32(&sh->p_full[s >> 1][s & 1]), 128);
+      tc::mbar_init(tc::smem_u32(&sh->o_done[s >> 1][s & 1]), 1);
+    }
+    sh->abort = 0;
+    sh->poison = 0;
+    sh->max_hi = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == NB * 4 + 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&sh->tmem_base)), "r"(TM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  __syncthreads();
+  if (warp < NB * 4) {
+    // query rows: a lane takes sixteen dims, HD / 16 lanes a row
+    constexpr int LPR = HD / 16;
+#pragma unroll 1
+    for (int e = 0; e < LPR; ++e) {
+      const int qrow = (int)threadIdx.x / LPR + e * (NB * 128 / LPR), j = threadIdx.x % LPR;
+      const int pp = pair0 + qrow;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      if (pp < Pn) {
+        const long long off = (long long)(pp / Gq) * p.q_stride + (long long)(kvh * Gq + pp % Gq) * HD + j * 16;
+        if (p.q_bf16) load16((const bf16*)p.q + off, x);
+        else load16((const float*)p.q + off, x);
+      }
+      const RowScale rs = row_scale<16, LPR>(x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = x[i] * rs.up1 * rs.up2;
+      uint8_t* dst = smem + (qrow / TP) * Q_BYTES + (j >> 2) * HALF_Q + (qrow % TP) * 128;
+      const int c = (j & 3) * 2, sw = qrow & 7;
+      *reinterpret_cast<uint4*>(dst + ((c ^ sw) << 4)) = halves8(x);
+      *reinterpret_cast<uint4*>(dst + (((c + 1) ^ sw) << 4)) = halves8(x + 8);
+      if (j == 0) sh->mult[qrow] = rs.mult * rsqrtf((float)HD);
+    }
+    const int pp = pair0 + (int)threadIdx.x;
+    if (pp < Pn) atomicMax(&sh->max_hi, row_limit(p, pp / Gq));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = sh->tmem_base;
+  // key tiles of this CTA: the cache's, then the own rows'
+  const int n_cache = sh->max_hi;
+  const int own_lo = p.own_n > 0 ? r_lo / p.T * p.T : 0;
+  const int nt_c = (n_cache + TK - 1) / TK, nt_all = nt_c + (p.own_n > 0 ? (r_hi - own_lo) / TK + 1 : 0);
+  const int t_lo = (int)((long long)nt_all * split / p.splits), nt = (int)((long long)nt_all * (split + 1) / p.splits) - t_lo;
+
+  if (warp >= NB * 4 && warp < NB * 4 + 4) {
+    // ---- tiles in the order the multiplies take them: K0, K1, V0, K2, V1, ...  A thread takes half a row of a tile: key
+    // tid % 64 (eight neighbours fill eight different 16-byte columns of the swizzle).  Codes are fetched three tiles ahead.
+    constexpr int W = HD / 16;                       // words of codes per thread
+    const int tid = (int)threadIdx.x - NB * 128, row = tid & 63, part = tid >> 6;
+    struct Piece { uint32_t w[W], s; };
+    const int n_items = 2 * nt;
+    auto item = [&](int i, bool& value, int& t) {    // item i of the order
+      value = i > 0 && (i == n_items - 1 || (i & 1) == 0);
+      t = i == 0 ? 0 : (i == n_items - 1 ? nt - 1 : (value ? (i - 2) / 2 : (i + 1) / 2));
+    };
+    auto fetch = [&](Piece& d, int i) {
+      bool value;
+      int t;
+      item(i, value, t);
+      const int tt = t_lo + t;
+      const bool own = tt >= nt_c;
+      const View& v = own ? (value ? p.own_v : p.own_k) : (value ? p.v : p.k);
+      const int key = own ? own_lo + (tt - nt_c) * TK + row : tt * TK + row;
+      const bool in = own ? key <= r_hi : key < n_cache;
+      const long long pos = own ? p.own_pos0 + key : key;
+      d.s = 0;
+#pragma unroll
+      for (int k = 0; k < W; ++k) d.w[k] = 0x88888888u;
+      if (in) {
+        const uint8_t* c = v.codes + kvh * v.head_codes + pos * (HD / 2) + part * (HD / 4);
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k) {
+          const uint4 u = __ldg(reinterpret_cast<const uint4*>(c) + k);
+          d.w[4 * k] = u.x; d.w[4 * k + 1] = u.y; d.w[4 * k + 2] = u.z; d.w[4 * k + 3] = u.w;
+        }
+        const uint8_t* x = v.scales + kvh * v.head_scales + pos * (HD / BLOCK) + part * (HD / 32);
+        if constexpr (HD == 128) d.s = __ldg(reinterpret_cast<const uint32_t*>(x));
+        else d.s = __ldg(reinterpret_cast<const unsigned short*>(x));
+      }
+    };
+    bool ok = true;
+    auto convert = [&](Piece& d, int i) {
+      const uint32_t s = (uint32_t)i % RING;
+      ok = tc::mbar_wait(tc::smem_u32(&sh->empty[s]), (((uint32_t)i / RING) & 1u) ^ 1u, p.status, p.spin_fast, p.spin_slow);
+      if (!ok) return;
+      bool value;
+      int t;
+      item(i, value, t);
+      if (value && __vcmpeq4(d.s, 0xffffffffu)) {
+        sh->poison = 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (((d.s >> (8 * k)) & 255u) == NAN_SCALE) d.s &= ~(255u << (8 * k));
+      }
+      uint8_t* dst = smem + NB * Q_BYTES + s * KV_BYTES + (HD == 128 ? part * HALF_KV : 0) + row * 128;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const uint32_t sb = (d.s >> (8 * (k >> 1))) & 255u;
+        const Scale2 sc = scale2(sb, sb);
+        const uint32_t w = d.w[k], w8 = w >> 8;
+        const int c = HD == 128 ? k : part * 4 + k;
+        *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) =
+            make_uint4(nib_lo(w, sc), nib_hi(w, sc), nib_lo(w8, sc), nib_hi(w8, sc));
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->full[s])) : "memory");
+    };
+    Piece d[4];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < n_items) fetch(d[k], k);
+#pragma unroll 1
+    for (int i = 0; i < n_items && ok; i += 4) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i + k < n_items && ok) {
+          if (i + k + 3 < n_items) fetch(d[(k + 3) & 3], i + k + 3);
+          convert(d[k], i + k);
+        }
+      }
+    }
+    if (!ok) sh->abort = 1;
+  } else if (warp == NB * 4 + 4) {
+    // ---- multiplies.  Both operands half precision, fp32 accumulators.
+    const uint32_t idesc_qk = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
+    const uint32_t idesc_pv = (1u << 4) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
+    const uint32_t el = wide::elect_one();
+    uint32_t n = 0;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = tc::mbar_wait(tc::smem_u32(bar), parity, p.status, p.spin_fast, p.spin_slow);
+      ok = __all_sync(0xffffffffu, ok);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      return ok;
+    };
+    auto scores = [&](int t) {
+      const uint32_t s = n % RING;
+      if (!wait(&sh->full[s], (n / RING) & 1u)) return;
+      const uint32_t k_base = base + NB * Q_BYTES + s * KV_BYTES;
+#pragma unroll
+      for (int bl = 0; bl < NB; ++bl) {
+        const uint32_t d = tmem + bl * 128 + (t & 1) * TK;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint64_t da = tc::make_smem_desc(base + bl * Q_BYTES + (k >> 2) * HALF_Q) + (uint64_t)((k & 3) * 2);
+          const uint64_t db = tc::make_smem_desc(k_base + (k >> 2) * HALF_KV) + (uint64_t)((k & 3) * 2);
+          wide::mma_ss(d, da, db, idesc_qk, k > 0, el);
+        }
+        wide::commit_one(tc::smem_u32(&sh->s_full[bl][t & 1]), el);
+      }
+      wide::commit_one(tc::smem_u32(&sh->empty[s]), el);
+      ++n;
+    };
+    if (nt > 0) scores(0);
+    for (int t = 0; t < nt && ok; ++t) {
+      if (t + 1 < nt) scores(t + 1);   // (buffer of tile t - 1: its P V was issued before, the tensor pipe keeps the order)
+      const uint32_t s = n % RING;
+      if (!ok || !wait(&sh->full[s], (n / RING) & 1u)) break;
+      const uint32_t v_base = base + NB * Q_BYTES + s * KV_BYTES;
+      // V tile: key rows of 64 dims, the MN-major form of B (64-dim halves HALF_KV apart)
+      const uint64_t db = (tc::make_smem_desc(v_base) & ~(0x3FFFull << 16)) | ((uint64_t)(HALF_KV / 16) << 16);
+#pragma unroll
+      for (int bl = 0; bl < NB; ++bl) {
+        if (!wait(&sh->p_full[bl][t & 1], (t >> 1) & 1u)) break;
+        const uint32_t a = tmem + bl * 128 + (t & 1) * TK;
+#pragma unroll
+        for (int k = 0; k < TK / 16; ++k)
+          wide::mma_ts(tmem + O_COL + bl * 128, a + k * 8, db + (uint64_t)(k * 128), idesc_pv, t > 0 || k > 0, el);
+        wide::commit_one(tc::smem_u32(&sh->o_done[bl][t & 1]), el);
+      }
+      if (!ok) break;
+      wide::commit_one(tc::smem_u32(&sh->empty[s]), el);
+      ++n;
+    }
+    if (!ok) sh->abort = 1;
+  } else {
+    // ---- softmax: a thread per pair
+    const int bl = warp >> 2, pp = pair0 + (int)threadIdx.x;
+    const bool pv = pp < Pn;
+    const int r = pv ? pp / Gq : 0, hq = kvh * Gq + (pv ? pp % Gq : 0);
+    const int own_first = r / p.T * p.T, lim = pv ? row_limit(p, r) : 0;
+    const float mult = lim > 0 || p.own_n > 0 ? sh->mult[threadIdx.x] : 1.f;   // (a row that sees nothing: zeros whatever its query)
+    const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + bl * 128;
+    const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + O_COL + bl * 128;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int t = 0; t < nt; ++t) {
+      ok = tc::mbar_wait(tc::smem_u32(&sh->s_full[bl][t & 1]), (t >> 1) & 1u, p.status, p.spin_fast, p.spin_slow);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      float s[TK];
+      const uint32_t t_s = t_row + (t & 1) * TK;
+      {
+        float a[32], c[32];
+        wide::tmem_ld<32>(t_s, a);
+        wide::tmem_ld<32>(t_s + 32, c);
+        wide::tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 32; ++k) { s[k] = a[k]; s[32 + k] = c[k]; }
+      }
+      // visible keys of the tile: [lo, hi)
+      const int tt = t_lo + t;
+      int lo = 0, hi = TK;
+      if (tt < nt_c) {
+        hi = min(TK, lim - tt * TK);
+      } else {
+        const int y = own_lo + (tt - nt_c) * TK;
+        lo = max(0, own_first - y);
+        hi = min(TK, r + 1 - y);
+      }
+      if (!pv) hi = 0;
+      if (__any_sync(0xffffffffu, lo > 0 || hi < TK)) {
+#pragma unroll
+        for (int k = 0; k < TK; ++k)
+          if (k < lo || k >= hi) s[k] = -INFINITY;
+      }
+      float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int k = 0; k < TK; ++k) m4[k & 3] = fmaxf(m4[k & 3], s[k]);
+      float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+      mx = mx == -INFINITY ? mx : mx * mult;          // (no visible key: -inf whatever the factor)
+      const bool grow = t > 0 && mx > m + LAZY;       // (also the first visible key of the row: m = -inf)
+      if (t == 0) {
+        m = mx;
+      } else if (__any_sync(0xffffffffu, grow)) {
+        // the outputs so far are rescaled: every P V issued so far (tile t - 1 is the last) has to be done
+        ok = tc::mbar_wait(tc::smem_u32(&sh->o_done[bl][(t - 1) & 1]), ((t - 1) >> 1) & 1u, p.status, p.spin_fast, p.spin_slow);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const float corr = grow ? exp2f(m - mx) : 1.f;
+        if (grow) { l *= corr; m = mx; }
+#pragma unroll 1
+        for (int c = 0; c < HD; c += 32) {
+          float o[32];
+          wide::tmem_ld<32>(t_o + c, o);
+          wide::tmem_wait_ld();
+          uint32_t u[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) u[k] = __float_as_uint(o[k] * corr);
+          wide::tmem_st32(t_o + c, u);
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      }
+      const float mm = m == -INFINITY ? 0.f : m - MANY_BITS;   // no visible key so far: all weights are exp2(-inf) = 0
+      float r4[4] = {0.f, 0.f, 0.f, 0.f};
+      uint32_t ph[32];
+#pragma unroll
+      for (int k = 0; k < TK; k += 2) {
+        const float a = ex2(fmaf(s[k], mult, -mm)), c = ex2(fmaf(s[k + 1], mult, -mm));
+        r4[(k >> 1) & 3] += a + c;
+        ph[k >> 1] = pack_half(a, c);
+      }
+      l += (r4[0] + r4[1]) + (r4[2] + r4[3]);
+      wide::tmem_st32(t_s, ph);
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->p_full[bl][t & 1])) : "memory");
+    }
+    if (ok && nt > 0) {
+      ok = tc::mbar_wait(tc::smem_u32(&sh->o_done[bl][(nt - 1) & 1]), ((nt - 1) >> 1) & 1u, p.status, p.spin_fast, p.spin_slow);
+      ok = __all_sync(0xffffffffu, ok);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    if (!ok) sh->abort = 1;
+    if (ok) {
+      // (poison was written before the last tile's barrier; NaN blocks among the keys this pair sees)
+      uint32_t bad = 0;
+      if (*(volatile int*)&sh->poison && pv) {
+        const uint8_t* xc = p.v.scales + kvh * p.v.head_scales;
+        const uint8_t* xo = p.own_v.scales + kvh * p.own_v.head_scales;
+        const int k0 = t_lo * TK, k1 = min(lim, (t_lo + nt) * TK);
+        for (int k = k0; k < k1; ++k)
+#pragma unroll 1
+          for (int j = 0; j < HD / BLOCK; ++j) bad |= (uint32_t)(xc[(long long)k * (HD / BLOCK) + j] == NAN_SCALE) << j;
+        if (t_lo + nt > nt_c && p.own_n > 0)
+          for (int k = max(own_first, own_lo + max(0, t_lo - nt_c) * TK); k <= min(r, own_lo + (t_lo + nt - nt_c) * TK - 1); ++k)
+#pragma unroll 1
+            for (int j = 0; j < HD / BLOCK; ++j)
+              bad |= (uint32_t)(xo[(p.own_pos0 + k) * (HD / BLOCK) + j] == NAN_SCALE) << j;
+      }
+      const bool part = p.splits > 1;
+      const float inv = part ? 1.f : (l == 0.f ? 0.f : 1.0f / l);
+      const long long idx = ((long long)r * p.nq + hq) * p.splits + split;
+#pragma unroll 1
+      for (int c = 0; c < HD; c += 32) {
+        float o[32];
+        if (nt > 0) {
+          wide::tmem_ld<32>(t_o + c, o);
+          wide::tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0.f;
+        }
+        float f[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const int dim = (k & ~7) + ((k & 1) << 2) + ((k & 7) >> 1);   // columns hold dims 0 4 1 5 2 6 3 7 of each eight
+          f[dim] = ((bad >> ((c + k) >> 4)) & 1u) ? __int_as_float(0x7fffffff) : o[k] * inv;
+        }
+        if (!part) {
+          bf16* dst = (bf16*)p.out + (long long)r * p.out_stride + (long long)hq * HD + c;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            wide::st16b(dst + 8 * k, pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]),
+                        pack_bf16(f[8 * k + 4], f[8 * k + 5]), pack_bf16(f[8 * k + 6], f[8 * k + 7]), pv);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) wide::st8(p.part + idx * HD + c + 8 * k, f + 8 * k, true, pv);
+        }
+      }
+      if (pv && part) p.part_ml[idx] = make_float2(m, l);
+    }
+  }
+
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (sh->abort)
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  if (warp == NB * 4 + 4) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TM_COLS) : "memory");
+  }
+}
+
+// The parts of a (row, query head), in their order: a warp each.
+template <int HD>
+__global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ AttnArgs p) {
+  const long long rh = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (rh >= (long long)p.R * p.nq) return;
+  const int lane = threadIdx.x & 31, parts = p.splits;
+  constexpr int E = HD / 32;
+  const float2* ml = p.part_ml + rh * parts;
+  float mx = -INFINITY;
+  for (int i = 0; i < parts; ++i) mx = fmaxf(mx, __ldcg(&ml[i]).x);
+  float den = 0.f, a[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) a[e] = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) {
+    const float2 v = __ldcg(&ml[i]);
+    const float w = v.x == -INFINITY ? (v.y == 0.f ? 0.f : 1.f) : exp2f(v.x - mx);   // (a sum without a maximum is 0, or NaN)
+    den = fmaf(v.y, w, den);
+    const float* src = p.part + (rh * parts + i) * HD + lane * E;
+    if constexpr (E == 4) {
+      const float4 u = __ldcg(reinterpret_cast<const float4*>(src));
+      a[0] = fmaf(w, u.x, a[0]); a[1] = fmaf(w, u.y, a[1]); a[2] = fmaf(w, u.z, a[2]); a[3] = fmaf(w, u.w, a[3]);
+    } else {
+      const float2 u = __ldcg(reinterpret_cast<const float2*>(src));
+      a[0] = fmaf(w, u.x, a[0]); a[1] = fmaf(w, u.y, a[1]);
+    }
+  }
+  const float inv = den == 0.f ? 0.f : 1.0f / den;
+  bf16* dst = (bf16*)p.out + rh / p.nq * p.out_stride + rh % p.nq * HD + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; e += 2) reinterpret_cast<uint32_t*>(dst)[e >> 1] = pack_bf16(a[e] * inv, a[e + 1] * inv);
 }
 
 }  // namespace kv4

@@ -202,6 +202,20 @@ def test_rows_with_their_own_keys(heads, dtype, S, T, ctx, own_at):
     attend_case(heads, dtype, S, T, ctx, True, False, seed=S * 100 + T, own_at=own_at)
 
 
+@pytest.mark.parametrize("heads", [(32, 8, 128), (8, 2, 64), (12, 4, 128), (8, 1, 128)])
+@pytest.mark.parametrize("T,ctx", [(17, 0), (17, 1), (33, 63), (64, 64), (65, 65), (129, 10), (200, 333)])
+def test_many_rows(heads, T, ctx):
+    """Prompt chunks: blocks of pairs and tiles of keys that end anywhere, whole and cut into parts."""
+    attend_case(heads, "bf16", 1, T, ctx, True, False, seed=T + ctx, max_rows=T + 1)
+    if ctx:
+        attend_case(heads, "bf16", 1, T, ctx, False, False, seed=T + ctx + 1)
+
+
+def test_a_prompt_of_many_blocks():
+    attend_case((32, 8, 128), "bf16", 1, 1100, 5, True, False, seed=9)
+    attend_case((8, 2, 64), "bf16", 2, 600, 70, True, False, seed=10)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("heads,R,ctx", [((32, 8, 128), 6, 300), ((4, 2, 64), 33, 1000), ((12, 4, 128), 100, 130), ((8, 1, 128), 1, 40)])
 @pytest.mark.parametrize("own", [False, True])
@@ -226,7 +240,8 @@ def test_flat_and_peaked_rows(dtype, qscale):
     attend_case((8, 2, 128), dtype, 1, 3, 200, True, False, seed=8, qscale=qscale)
 
 
-def test_a_growing_maximum():
+@pytest.mark.parametrize("R", [2, 40])
+def test_a_growing_maximum(R):
     """Scores that rise along the keys move the running maximum at every step."""
     heads, cap = (8, 2, 128), 600
     eng, kv = make(heads, cap)
@@ -235,12 +250,12 @@ def test_a_growing_maximum():
     k = k.bfloat16()
     v = rows(2, (512, 2, 128), "bf16")
     kk, vv = set_cache(kv, heads, cap, k, v)
-    q = torch.zeros((2, 8, 128))
+    q = torch.zeros((R, 8, 128))
     q[..., 0] = 20.0
-    q[1, ..., 0] = -20.0
+    q[1::2, ..., 0] = -20.0
     q = q.bfloat16()
     out = eng.kv4_attention(q.cuda(), kv, 512)
-    want, spread, vmax = ref.attention(ref.to_np(q), kk, vv, ref.seen_mask(2, 1, 512, False))
+    want, spread, vmax = ref.attention(ref.to_np(q), kk, vv, ref.seen_mask(R, 1, 512, False))
     assert (np.abs(ref.to_np(out) - want) <= ref.tolerance(want, spread, vmax, True)).all()
 
 
@@ -272,15 +287,17 @@ def test_nan_blocks_reach_the_rows_that_see_them_only(dtype, T):
     assert bool((nan == want).all())
 
 
-def test_a_query_that_is_not_finite():
+@pytest.mark.parametrize("R", [3, 50])
+def test_a_query_that_is_not_finite(R):
     heads = (8, 2, 128)
     eng, kv = make(heads, 64)
     k, v = rows(1, (50, 2, 128), "bf16"), rows(2, (50, 2, 128), "bf16")
     set_cache(kv, heads, 64, k, v)
-    q = rows(3, (3, 8, 128), "bf16")
+    q = rows(3, (R, 8, 128), "bf16")
     q[1, 2, 9] = float("inf")
     q[2, 5, 0] = float("nan")
-    vis = torch.tensor([50, 50, 0], dtype=torch.int32)
+    vis = torch.full((R,), 50, dtype=torch.int32)
+    vis[2] = 0
     out = eng.kv4_attention(q.cuda(), kv, 50, visible=vis.cuda())
     nan = torch.isnan(out).cpu()
     want = torch.zeros_like(nan)
@@ -364,6 +381,32 @@ def test_positions_past_four_gigabytes():
         want = p @ vv[:, h] / (p.sum() + (cap - 20) * np.exp(-m))
         spread = (np.abs(kk[:, h]) @ np.abs(ref.to_np(q)[0, h])).max() / np.sqrt(128.0)
         assert (np.abs(out[0, h] - want) <= ref.tolerance(want, spread, np.abs(vv).max(), True)).all()
+
+
+@pytest.mark.parametrize("T", [20, 100])
+def test_waits_that_run_out_are_reported(T):
+    """The attention of many rows with a wait limit of a few polls: it ends by itself, the status says so once, and the next
+    call with the usual limit gives the same bits as before.  (A poll may itself last for microseconds, so a call may also get
+    through; the cache comes from memory to make that less likely.)"""
+    heads, ctx, cap = (32, 8, 128), 40000, 41000
+    eng, kv = make(heads, cap, max_rows=128)
+    n_q, n_kv, hd = heads
+    eng.kv4_write(rows(1, (ctx + T, n_kv, hd), "bf16").cuda(), rows(2, (ctx + T, n_kv, hd), "bf16").cuda(), 0, kv)
+    q = rows(3, (T, n_q, hd), "bf16").cuda()
+    flush = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")
+    want = eng.kv4_attention(q, kv, ctx, T=T, own_pos0=ctx).clone()
+    assert eng.device_status() == 0
+    seen = []
+    for polls in (1, 1, 1, 2, 3, 20):
+        flush.zero_()
+        eng.set_wait_limit(polls)
+        eng.kv4_attention(q, kv, ctx, T=T, own_pos0=ctx)
+        seen.append(eng.device_status())
+        assert seen[-1] in (0, -6)
+        eng.set_wait_limit(0)
+        assert eng.device_status() == 0
+        assert torch.equal(eng.kv4_attention(q, kv, ctx, T=T, own_pos0=ctx), want)
+    print("status under 1, 1, 1, 2, 3, 20 polls:", seen)
 
 
 # ------------------------------------------------------------------ refusals
