@@ -284,6 +284,26 @@ __device__ __forceinline__ RowScale row_scale(const float (&x)[N]) {
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
 // Scales of the two halves of a register, as the conversion needs them.
 struct Scale2 {
   __half2 s, s16, m72;   // s, s / 16, -72 s
@@ -705,7 +725,7 @@ constexpr float LAZY = 5.f, MANY_BITS = 10.f;   // the maximum moves when exceed
 template <int HD, int NB>
 constexpr int many_smem() { return NB * TP * HD * 2 + RING * TK * HD * 2 + 2048; }
 template <int NB>
-constexpr int many_threads() { return NB * 128 + 128 + 32; }
+constexpr int many_threads() { return NB * 128 + 128 + NB * 32; }
 
 struct ManyShared {
   uint64_t full[RING], empty[RING], s_full[2][2], p_full[2][2];
@@ -750,12 +770,12 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < RING; ++s) {
-      tc::mbar_init(tc::smem_u32(&sh->full[s]), 128);
-      tc::mbar_init(tc::smem_u32(&sh->empty[s]), 1);
+      tc::mbar_init(tc::smem_u32(&sh->full[s]), 4);
+      tc::mbar_init(tc::smem_u32(&sh->empty[s]), NB);
     }
     for (int s = 0; s < 4; ++s) {
       tc::mbar_init(tc::smem_u32(&sh->s_full[s >> 1][s & 1]), 1);
-      tc::mbar_init(tc::smem_u32(&sh->p_full[s >> 1][s & 1]), 128);
+      tc::mbar_init(tc::smem_u32(&sh->p_full[s >> 1][s & 1]), 4);
       tc::mbar_init(tc::smem_u32(&sh->o_done[s >> 1][s & 1]), 1);
     }
     sh->abort = 0;
@@ -808,135 +828,135 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
   const int nt_c = (n_cache + TK - 1) / TK, nt_all = nt_c + (p.own_n > 0 ? (r_hi - own_lo) / TK + 1 : 0);
   const int t_lo = (int)((long long)nt_all * split / p.splits), nt = (int)((long long)nt_all * (split + 1) / p.splits) - t_lo;
 
+  // A wait of a whole warp.  The first poll stands outside the bounded loop: most waits here find their phase complete, and the
+  // loop's code cost each of them about 200 cycles of the tile's chain.
+  bool ok = true;
+  auto warp_wait = [&](uint64_t* bar, uint32_t parity) {
+    if (!__all_sync(0xffffffffu, tc::mbar_test(tc::smem_u32(bar), parity))) {
+      ok = tc::mbar_wait(tc::smem_u32(bar), parity, p.status, p.spin_fast, p.spin_slow);
+      ok = __all_sync(0xffffffffu, ok);
+    }
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    return ok;
+  };
+
   if (warp >= NB * 4 && warp < NB * 4 + 4) {
     // ---- tiles in the order the multiplies take them: K0, K1, V0, K2, V1, ...  A thread takes half a row of a tile: key
-    // tid % 64 (eight neighbours fill eight different 16-byte columns of the swizzle).  Codes are fetched three tiles ahead.
+    // tid % 64 (eight neighbours fill eight different 16-byte columns of the swizzle).  Codes are fetched two tiles ahead.
     constexpr int W = HD / 16;                       // words of codes per thread
     const int tid = (int)threadIdx.x - NB * 128, row = tid & 63, part = tid >> 6;
     struct Piece { uint32_t w[W], s; };
-    const int n_items = 2 * nt;
-    auto item = [&](int i, bool& value, int& t) {    // item i of the order
-      value = i > 0 && (i == n_items - 1 || (i & 1) == 0);
-      t = i == 0 ? 0 : (i == n_items - 1 ? nt - 1 : (value ? (i - 2) / 2 : (i + 1) / 2));
+    struct Source { const uint8_t *c, *x; };         // this thread's share of key 0
+    auto source = [&](const View& v, long long pos) {
+      return Source{v.codes + kvh * v.head_codes + pos * (HD / 2) + part * (HD / 4),
+                    v.scales + kvh * v.head_scales + pos * (HD / BLOCK) + part * (HD / 32)};
     };
-    auto fetch = [&](Piece& d, int i) {
-      bool value;
-      int t;
-      item(i, value, t);
-      const int tt = t_lo + t;
-      const bool own = tt >= nt_c;
-      const View& v = own ? (value ? p.own_v : p.own_k) : (value ? p.v : p.k);
-      const int key = own ? own_lo + (tt - nt_c) * TK + row : tt * TK + row;
-      const bool in = own ? key <= r_hi : key < n_cache;
-      const long long pos = own ? p.own_pos0 + key : key;
+    const Source src[2][2] = {{source(p.k, 0), source(p.own_k, p.own_pos0)}, {source(p.v, 0), source(p.own_v, p.own_pos0)}};
+    auto fetch = [&](Piece& d, const Source (&sv)[2], int t) {
+      const bool own = t_lo + t >= nt_c;
+      const int key = (own ? own_lo - nt_c * TK : 0) + (t_lo + t) * TK + row, end = own ? r_hi + 1 : n_cache;
       d.s = 0;
 #pragma unroll
       for (int k = 0; k < W; ++k) d.w[k] = 0x88888888u;
-      if (in) {
-        const uint8_t* c = v.codes + kvh * v.head_codes + pos * (HD / 2) + part * (HD / 4);
+      if (t < nt && key < end) {
+        const uint8_t* c = (own ? sv[1].c : sv[0].c) + (long long)key * (HD / 2);
+        const uint8_t* x = (own ? sv[1].x : sv[0].x) + (long long)key * (HD / BLOCK);
 #pragma unroll
         for (int k = 0; k < W / 4; ++k) {
           const uint4 u = __ldg(reinterpret_cast<const uint4*>(c) + k);
           d.w[4 * k] = u.x; d.w[4 * k + 1] = u.y; d.w[4 * k + 2] = u.z; d.w[4 * k + 3] = u.w;
         }
-        const uint8_t* x = v.scales + kvh * v.head_scales + pos * (HD / BLOCK) + part * (HD / 32);
         if constexpr (HD == 128) d.s = __ldg(reinterpret_cast<const uint32_t*>(x));
         else d.s = __ldg(reinterpret_cast<const unsigned short*>(x));
       }
     };
-    bool ok = true;
-    auto convert = [&](Piece& d, int i) {
-      const uint32_t s = (uint32_t)i % RING;
-      ok = tc::mbar_wait(tc::smem_u32(&sh->empty[s]), (((uint32_t)i / RING) & 1u) ^ 1u, p.status, p.spin_fast, p.spin_slow);
-      if (!ok) return;
-      bool value;
-      int t;
-      item(i, value, t);
+    uint32_t slot = 0, phase = 1;                    // (the first pass finds every slot free)
+    const uint32_t dst0 = base + NB * Q_BYTES + (HD == 128 ? part * HALF_KV : 0) + row * 128;
+    const uint32_t col0 = (uint32_t)((row & 7) << 4) ^ (HD == 128 ? 0u : (uint32_t)part * 64u);
+    auto convert = [&](Piece& d, bool value) {
+      if (!warp_wait(&sh->empty[slot], phase)) return;
       if (value && __vcmpeq4(d.s, 0xffffffffu)) {
         sh->poison = 1;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if (((d.s >> (8 * k)) & 255u) == NAN_SCALE) d.s &= ~(255u << (8 * k));
       }
-      uint8_t* dst = smem + NB * Q_BYTES + s * KV_BYTES + (HD == 128 ? part * HALF_KV : 0) + row * 128;
+      const uint32_t dst = dst0 + slot * KV_BYTES;
 #pragma unroll
       for (int k = 0; k < W; ++k) {
         const uint32_t sb = (d.s >> (8 * (k >> 1))) & 255u;
         const Scale2 sc = scale2(sb, sb);
         const uint32_t w = d.w[k], w8 = w >> 8;
-        const int c = HD == 128 ? k : part * 4 + k;
-        *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) =
-            make_uint4(nib_lo(w, sc), nib_hi(w, sc), nib_lo(w8, sc), nib_hi(w8, sc));
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (col0 ^ (uint32_t)(k << 4))), "r"(nib_lo(w, sc)),
+                     "r"(nib_hi(w, sc)), "r"(nib_lo(w8, sc)), "r"(nib_hi(w8, sc))
+                     : "memory");
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->full[s])) : "memory");
+      __syncwarp();
+      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->full[slot])) : "memory");
+      if (++slot == RING) { slot = 0; phase ^= 1u; }
     };
-    Piece d[4];
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (k < n_items) fetch(d[k], k);
+    Piece dk[3], dv[3];
+    if (nt > 0) {
+      fetch(dk[0], src[0], 0);
+      fetch(dk[1], src[0], 1);
+      fetch(dv[0], src[1], 0);
+      fetch(dk[2], src[0], 2);
+      fetch(dv[1], src[1], 1);
+      convert(dk[0], false);
+    }
 #pragma unroll 1
-    for (int i = 0; i < n_items && ok; i += 4) {
+    for (int t = 0; t < nt && ok; t += 3) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (i + k < n_items && ok) {
-          if (i + k + 3 < n_items) fetch(d[(k + 3) & 3], i + k + 3);
-          convert(d[k], i + k);
+      for (int k = 0; k < 3; ++k) {
+        if (t + k < nt && ok) {
+          fetch(dk[k], src[0], t + k + 3);
+          fetch(dv[(k + 2) % 3], src[1], t + k + 2);
+          if (t + k + 1 < nt) convert(dk[(k + 1) % 3], false);
+          if (ok) convert(dv[k], true);
         }
       }
     }
     if (!ok) sh->abort = 1;
-  } else if (warp == NB * 4 + 4) {
-    // ---- multiplies.  Both operands half precision, fp32 accumulators.
+  } else if (warp >= NB * 4 + 4) {
+    // ---- multiplies: a warp per block of pairs, so that one's waits are covered by the other's multiplies (one warp for both:
+    // 2350 cycles per tile of 2 x 128 pairs, of which the tensor pipe worked 1280).  Both operands half precision, fp32 accumulators.
+    const int bl = warp - (NB * 4 + 4);
     const uint32_t idesc_qk = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
     const uint32_t idesc_pv = (1u << 4) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
     const uint32_t el = wide::elect_one();
-    uint32_t n = 0;
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = tc::mbar_wait(tc::smem_u32(bar), parity, p.status, p.spin_fast, p.spin_slow);
-      ok = __all_sync(0xffffffffu, ok);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      return ok;
+    const uint32_t t_s = tmem + bl * 128, t_o = tmem + O_COL + bl * 128;
+    const uint32_t q_base = base + bl * Q_BYTES;
+    uint32_t slot = 0, phase = 0;
+    auto next = [&]() {
+      if (++slot == RING) { slot = 0; phase ^= 1u; }
     };
     auto scores = [&](int t) {
-      const uint32_t s = n % RING;
-      if (!wait(&sh->full[s], (n / RING) & 1u)) return;
-      const uint32_t k_base = base + NB * Q_BYTES + s * KV_BYTES;
+      if (!warp_wait(&sh->full[slot], phase)) return;
+      const uint32_t k_base = base + NB * Q_BYTES + slot * KV_BYTES, d = t_s + (t & 1) * TK;
 #pragma unroll
-      for (int bl = 0; bl < NB; ++bl) {
-        const uint32_t d = tmem + bl * 128 + (t & 1) * TK;
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint64_t da = tc::make_smem_desc(base + bl * Q_BYTES + (k >> 2) * HALF_Q) + (uint64_t)((k & 3) * 2);
-          const uint64_t db = tc::make_smem_desc(k_base + (k >> 2) * HALF_KV) + (uint64_t)((k & 3) * 2);
-          wide::mma_ss(d, da, db, idesc_qk, k > 0, el);
-        }
-        wide::commit_one(tc::smem_u32(&sh->s_full[bl][t & 1]), el);
+      for (int k = 0; k < HD / 16; ++k) {
+        const uint64_t da = tc::make_smem_desc(q_base + (k >> 2) * HALF_Q) + (uint64_t)((k & 3) * 2);
+        const uint64_t db = tc::make_smem_desc(k_base + (k >> 2) * HALF_KV) + (uint64_t)((k & 3) * 2);
+        wide::mma_ss(d, da, db, idesc_qk, k > 0, el);
       }
-      wide::commit_one(tc::smem_u32(&sh->empty[s]), el);
-      ++n;
+      wide::commit_one(tc::smem_u32(&sh->s_full[bl][t & 1]), el);
+      wide::commit_one(tc::smem_u32(&sh->empty[slot]), el);
+      next();
     };
     if (nt > 0) scores(0);
     for (int t = 0; t < nt && ok; ++t) {
       if (t + 1 < nt) scores(t + 1);   // (buffer of tile t - 1: its P V was issued before, the tensor pipe keeps the order)
-      const uint32_t s = n % RING;
-      if (!ok || !wait(&sh->full[s], (n / RING) & 1u)) break;
-      const uint32_t v_base = base + NB * Q_BYTES + s * KV_BYTES;
+      if (!ok || !warp_wait(&sh->full[slot], phase) || !warp_wait(&sh->p_full[bl][t & 1], (t >> 1) & 1u)) break;
       // V tile: key rows of 64 dims, the MN-major form of B (64-dim halves HALF_KV apart)
-      const uint64_t db = (tc::make_smem_desc(v_base) & ~(0x3FFFull << 16)) | ((uint64_t)(HALF_KV / 16) << 16);
+      const uint64_t db = (tc::make_smem_desc(base + NB * Q_BYTES + slot * KV_BYTES) & ~(0x3FFFull << 16)) |
+                          ((uint64_t)(HALF_KV / 16) << 16);
+      const uint32_t a = t_s + (t & 1) * TK;
 #pragma unroll
-      for (int bl = 0; bl < NB; ++bl) {
-        if (!wait(&sh->p_full[bl][t & 1], (t >> 1) & 1u)) break;
-        const uint32_t a = tmem + bl * 128 + (t & 1) * TK;
-#pragma unroll
-        for (int k = 0; k < TK / 16; ++k)
-          wide::mma_ts(tmem + O_COL + bl * 128, a + k * 8, db + (uint64_t)(k * 128), idesc_pv, t > 0 || k > 0, el);
-        wide::commit_one(tc::smem_u32(&sh->o_done[bl][t & 1]), el);
-      }
-      if (!ok) break;
-      wide::commit_one(tc::smem_u32(&sh->empty[s]), el);
-      ++n;
+      for (int k = 0; k < TK / 16; ++k) wide::mma_ts(t_o, a + k * 8, db + (uint64_t)(k * 128), idesc_pv, t > 0 || k > 0, el);
+      wide::commit_one(tc::smem_u32(&sh->o_done[bl][t & 1]), el);
+      wide::commit_one(tc::smem_u32(&sh->empty[slot]), el);
+      next();
     }
     if (!ok) sh->abort = 1;
   } else {
@@ -949,11 +969,8 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + bl * 128;
     const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + O_COL + bl * 128;
     float m = -INFINITY, l = 0.f;
-    bool ok = true;
     for (int t = 0; t < nt; ++t) {
-      ok = tc::mbar_wait(tc::smem_u32(&sh->s_full[bl][t & 1]), (t >> 1) & 1u, p.status, p.spin_fast, p.spin_slow);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      if (!warp_wait(&sh->s_full[bl][t & 1], (t >> 1) & 1u)) break;
       float s[TK];
       const uint32_t t_s = t_row + (t & 1) * TK;
       {
@@ -974,15 +991,20 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
         lo = max(0, own_first - y);
         hi = min(TK, r + 1 - y);
       }
-      if (!pv) hi = 0;
-      if (__any_sync(0xffffffffu, lo > 0 || hi < TK)) {
+      if (!pv) { lo = 0; hi = TK; }   // (nothing of these pairs is stored)
+      if (__any_sync(0xffffffffu, hi < TK)) {
 #pragma unroll
         for (int k = 0; k < TK; ++k)
-          if (k < lo || k >= hi) s[k] = -INFINITY;
+          if (k >= hi) s[k] = -INFINITY;
+      }
+      if (__any_sync(0xffffffffu, lo > 0)) {
+#pragma unroll
+        for (int k = 0; k < TK; ++k)
+          if (k < lo) s[k] = -INFINITY;
       }
       float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int k = 0; k < TK; ++k) m4[k & 3] = fmaxf(m4[k & 3], s[k]);
+      for (int k = 0; k < TK; k += 2) m4[(k >> 1) & 3] = max3(m4[(k >> 1) & 3], s[k], s[k + 1]);
       float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
       mx = mx == -INFINITY ? mx : mx * mult;          // (no visible key: -inf whatever the factor)
       const bool grow = t > 0 && mx > m + LAZY;       // (also the first visible key of the row: m = -inf)
@@ -990,9 +1012,7 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
         m = mx;
       } else if (__any_sync(0xffffffffu, grow)) {
         // the outputs so far are rescaled: every P V issued so far (tile t - 1 is the last) has to be done
-        ok = tc::mbar_wait(tc::smem_u32(&sh->o_done[bl][(t - 1) & 1]), ((t - 1) >> 1) & 1u, p.status, p.spin_fast, p.spin_slow);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (!warp_wait(&sh->o_done[bl][(t - 1) & 1], ((t - 1) >> 1) & 1u)) break;
         const float corr = grow ? exp2f(m - mx) : 1.f;
         if (grow) { l *= corr; m = mx; }
 #pragma unroll 1
@@ -1008,25 +1028,24 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       }
       const float mm = m == -INFINITY ? 0.f : m - MANY_BITS;   // no visible key so far: all weights are exp2(-inf) = 0
-      float r4[4] = {0.f, 0.f, 0.f, 0.f};
+      const float2 mult2 = make_float2(mult, mult), off2 = make_float2(-mm, -mm);
+      float2 r2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       uint32_t ph[32];
 #pragma unroll
       for (int k = 0; k < TK; k += 2) {
-        const float a = ex2(fmaf(s[k], mult, -mm)), c = ex2(fmaf(s[k + 1], mult, -mm));
-        r4[(k >> 1) & 3] += a + c;
-        ph[k >> 1] = pack_half(a, c);
+        const float2 x = fma2(make_float2(s[k], s[k + 1]), mult2, off2);
+        const float2 e = make_float2(ex2(x.x), ex2(x.y));
+        r2[(k >> 1) & 1] = add2(r2[(k >> 1) & 1], e);
+        ph[k >> 1] = pack_half(e.x, e.y);
       }
-      l += (r4[0] + r4[1]) + (r4[2] + r4[3]);
+      l += (r2[0].x + r2[0].y) + (r2[1].x + r2[1].y);
       wide::tmem_st32(t_s, ph);
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->p_full[bl][t & 1])) : "memory");
+      __syncwarp();
+      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->p_full[bl][t & 1])) : "memory");
     }
-    if (ok && nt > 0) {
-      ok = tc::mbar_wait(tc::smem_u32(&sh->o_done[bl][(nt - 1) & 1]), ((nt - 1) >> 1) & 1u, p.status, p.spin_fast, p.spin_slow);
-      ok = __all_sync(0xffffffffu, ok);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    }
+    if (ok && nt > 0) warp_wait(&sh->o_done[bl][(nt - 1) & 1], ((nt - 1) >> 1) & 1u);
     if (!ok) sh->abort = 1;
     if (ok) {
       // (poison was written before the last tile's barrier; NaN blocks among the keys this pair sees)
