@@ -626,11 +626,11 @@ int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
   // few blocks: their key tiles are split so that every SM has work
   const int items = p.blocks * p.nkv, keys = p.n_keys + (p.own_n > 0 ? std::min(p.own_n, NB * k4::TP + p.T) : 0);
   p.splits = std::max(1, std::min(ctx->num_sms / items, (keys + k4::TK - 1) / k4::TK));
-  if ((size_t)p.splits > 1 && (size_t)p.R * p.nq * p.splits > KV4_MANY_SLOTS) p.splits = 1;
+  p.splits = std::min(p.splits, std::max(1, (int)(KV4_MANY_SLOTS / ((size_t)items * NB * k4::TP))));
   k4::attn_many_kernel<HD, NB><<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
   int rc = launch_check(ctx);
   if (rc || p.splits == 1) return rc;
-  k4::merge_kernel<HD><<<(unsigned)(((long long)p.R * p.nq + 7) / 8), 256, 0, ctx->stream>>>(p);
+  k4::merge_kernel<HD, NB><<<items * (HD / 4) * NB / 2, 256, 0, ctx->stream>>>(p);
   return launch_check(ctx);
 }
 
@@ -660,8 +660,8 @@ int kv4_attend(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
   for (int r0 = 0; r0 < p.R_all; r0 += KV4_ROWS) {
     p.r0 = r0;
     p.R = std::min(KV4_ROWS, p.R_all - r0);
-    p.q = (const char*)q + r0 * p.q_stride * (p.q_bf16 ? 2 : 4);
-    p.out = (char*)out + r0 * p.out_stride * (p.out_bf16 ? 2 : 4);
+    p.q = (const char*)q + r0 * p.q_stride * (split ? 4 : 2);
+    p.out = (char*)out + r0 * p.out_stride * (split ? 4 : 2);
     int rc;
     if (c.head_dim == 128) rc = split ? kv4_rows_launch<128, true>(ctx, p) : kv4_rows_launch<128, false>(ctx, p);
     else rc = split ? kv4_rows_launch<64, true>(ctx, p) : kv4_rows_launch<64, false>(ctx, p);
@@ -684,13 +684,19 @@ int kv4_layer_attention(clasp_ctx* ctx, int S, int T, int C, int pos0, const cla
   p.own_v = write_kv ? p.v : kv4_view(ctx, ws.own_v, c.max_rows);
   p.own_pos0 = write_kv ? pos0 : 0;
   const long long units = (long long)R * (qkvd / (2 * k4::BLOCK));
-  k4::store_rows_kernel<<<(unsigned)((units + 255) / 256), 256, 0, ctx->stream>>>(ws.qkv, qkvd, ws.rope, R, T, c.n_q_heads,
-                                                                                c.n_kv_heads, c.head_dim, p.own_k, p.own_v,
-                                                                                p.own_pos0);
+  // the rotated queries wait in ws.attn, where the attention puts its result: a CTA reads its pairs' queries, no others,
+  // before it (or, of a split call, the one that adds the parts) writes theirs
+  const unsigned blocks = (unsigned)((units + 255) / 256);
+  if (c.dtype == CLASP_BF16)
+    k4::store_rows_kernel<bf16><<<blocks, 256, 0, ctx->stream>>>(ws.qkv, qkvd, ws.rope, R, T, c.n_q_heads, c.n_kv_heads,
+                                                                c.head_dim, p.own_k, p.own_v, p.own_pos0, (bf16*)ws.attn);
+  else
+    k4::store_rows_kernel<float><<<blocks, 256, 0, ctx->stream>>>(ws.qkv, qkvd, ws.rope, R, T, c.n_q_heads, c.n_kv_heads,
+                                                                 c.head_dim, p.own_k, p.own_v, p.own_pos0, (float*)ws.attn);
   int rc = launch_check(ctx);
   if (rc) return rc;
-  p.q = ws.qkv; p.q_stride = qkvd; p.q_bf16 = 0;
-  p.out = ws.attn; p.out_stride = c.n_q_heads * c.head_dim; p.out_bf16 = c.dtype == CLASP_BF16;
+  p.q = p.out = ws.attn;
+  p.q_stride = p.out_stride = c.n_q_heads * c.head_dim;
   p.R_all = R; p.T = T; p.n_keys = C; p.own_n = R;
   if (write_kv && pos0 == C) { p.causal = 1; p.n_keys = C + R; p.own_n = 0; }
   return kv4_attend(ctx, p);
@@ -1961,8 +1967,8 @@ int clasp_kv4_attention(clasp_ctx* ctx, const void* q, int64_t q_stride, int32_t
   if (R == 0) return CLASP_OK;
   if (!kv4_rows_ok(ctx, q, q_stride, c.n_q_heads) || !kv4_rows_ok(ctx, out, out_stride, c.n_q_heads)) return CLASP_ERR_INVALID_ARG;
   clasp::kv4::AttnArgs p{};
-  p.q = q; p.q_stride = q_stride; p.q_bf16 = c.dtype == CLASP_BF16;
-  p.out = out; p.out_stride = out_stride; p.out_bf16 = c.dtype == CLASP_BF16;
+  p.q = q; p.q_stride = q_stride;
+  p.out = out; p.out_stride = out_stride;
   p.R_all = (int)R; p.T = T; p.n_keys = ctx_len; p.visible = visible;
   p.k = p.own_k = kv4_view(ctx, kv->k, c.max_ctx);
   p.v = p.own_v = kv4_view(ctx, kv->v, c.max_ctx);

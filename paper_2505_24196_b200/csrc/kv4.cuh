@@ -153,20 +153,22 @@ __global__ void __launch_bounds__(256) read_kernel(View ck, View cv, int n, long
   store16((val ? v + row * v_stride : k + row * k_stride) + b * BLOCK, x);
 }
 
-// A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated in place, keys rotated and quantised, values
-// quantised.  Dims i and i + hd / 2 share a rotation, so a thread of the rotated part takes the blocks j and j + hd / 32.
-__global__ void __launch_bounds__(256) store_rows_kernel(float* __restrict__ qkv, long long ld, const float2* __restrict__ cs, int R,
-                                                         int T, int nq, int nkv, int hd, View ck, View cv, long long pos0) {
+// A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated and stored in the model dtype, keys rotated and
+// quantised, values quantised.  Dims i and i + hd / 2 share a rotation, so a thread of the rotated part takes the blocks j and j + hd / 32.
+template <typename T>
+__global__ void __launch_bounds__(256) store_rows_kernel(const float* __restrict__ qkv, long long ld, const float2* __restrict__ cs, int R,
+                                                         int rows, int nq, int nkv, int hd, View ck, View cv, long long pos0,
+                                                         T* __restrict__ q) {
   const int half_blocks = hd / (2 * BLOCK), per_row = (nq + 2 * nkv) * half_blocks;
   const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (u >= (long long)R * per_row) return;
   const int r = (int)(u / per_row), e = (int)(u - (long long)r * per_row), head = e / half_blocks, j = e - head * half_blocks;
-  float* p = qkv + r * ld + head * hd + j * BLOCK;
+  const float* p = qkv + r * ld + head * hd + j * BLOCK;
   float a[BLOCK], b[BLOCK];
   load16(p, a);
   load16(p + hd / 2, b);
   if (head < nq + nkv) {
-    const float2* w = cs + (long long)(r % T) * (hd / 2) + j * BLOCK;
+    const float2* w = cs + (long long)(r % rows) * (hd / 2) + j * BLOCK;   // (states of `rows` rows)
 #pragma unroll
     for (int i = 0; i < BLOCK; ++i) {
       const float2 c = w[i];
@@ -175,8 +177,9 @@ __global__ void __launch_bounds__(256) store_rows_kernel(float* __restrict__ qkv
       b[i] = y;
     }
     if (head < nq) {
-      store16(p, a);
-      store16(p + hd / 2, b);
+      T* out = q + ((long long)r * nq + head) * hd + j * BLOCK;
+      store16(out, a);
+      store16(out + hd / 2, b);
       return;
     }
   }
@@ -197,12 +200,10 @@ __global__ void __launch_bounds__(256) store_rows_kernel(float* __restrict__ qkv
 // own rows, the rows first..r of its state, which lie at own + own_pos0.  When the own rows continue the cache (a
 // verification: one state behind the context), the two are one prefix and own_n is 0: limit_r = prefix + r + 1.
 struct AttnArgs {
-  const void* q;           // row r, head h at q + r * q_stride + h * hd, float or bf16
+  const void* q;           // row r, head h at q + r * q_stride + h * hd; model dtype, as `out`
   long long q_stride;
-  int q_bf16;
   void* out;
   long long out_stride;
-  int out_bf16;
   int R, T, nq, nkv;
   View k, v;               // the cache
   int n_keys;              // positions any row may see
@@ -258,30 +259,30 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t o) {
   return y;
 }
 
-// A query row for half precision: the power of two (in two factors) that brings its largest magnitude into [2^13, 2^14), and
+// A query row for half precision: the power of two that brings its largest magnitude into [2^13, 2^14), and
 // the factor that takes it back and brings the scores into units of log2 (1 / sqrt(hd) aside).  LANES neighbouring lanes hold a row,
 // N values each.  A row with an infinity or NaN in it has no finite score: its factor is NaN, and so are all its weights.
 struct RowScale {
-  float up1, up2, mult;
+  float up, mult;
 };
+// a: the bits of the row's largest magnitude
+__device__ __forceinline__ RowScale scale_for(uint32_t a) {
+  const int up = 13 - max((int)(a >> 23) - 127, -113);   // rows far below 2^-113 are as good as zero
+  RowScale r;
+
+  r.up = __uint_as_float((uint32_t)(127 + up) << 23);
+  r.mult = __uint_as_float((uint32_t)(127 - up) << 23) * 1.4426950408889634f;
+  if (a >= 0x7f800000u) r.mult = __int_as_float(0x7fffffff);
+  return r;
+}
 template <int N, int LANES>
 __device__ __forceinline__ RowScale row_scale(const float (&x)[N]) {
-  float a = 0.f, bad = 0.f;
+  uint32_t a = 0;                      // magnitudes compare like their bits; infinities and NaN are the largest
 #pragma unroll
-  for (int e = 0; e < N; ++e) { a = fmaxf(a, fabsf(x[e])); bad += x[e] * 0.f; }
+  for (int e = 0; e < N; ++e) a = max(a, __float_as_uint(x[e]) & 0x7fffffffu);
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) {
-    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-    bad += __shfl_xor_sync(0xffffffffu, bad, o);
-  }
-  const int up = 13 - max((int)(__float_as_uint(a) >> 23) - 127, -113);   // rows far below 2^-113 are as good as zero
-  const int u1 = up >> 1, u2 = up - u1;
-  RowScale r;
-  r.up1 = __uint_as_float((uint32_t)(127 + u1) << 23);
-  r.up2 = __uint_as_float((uint32_t)(127 + u2) << 23);
-  r.mult = 1.4426950408889634f * __uint_as_float((uint32_t)(127 - u1) << 23) * __uint_as_float((uint32_t)(127 - u2) << 23);
-  if (bad != 0.f) r.mult = __int_as_float(0x7fffffff);
-  return r;
+  for (int o = LANES / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+  return scale_for(a);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -323,6 +324,14 @@ __device__ __forceinline__ uint32_t nib_lo(uint32_t w, const Scale2& s) {
 }
 __device__ __forceinline__ uint32_t nib_hi(uint32_t w, const Scale2& s) {
   return as_u32(__hfma2(as_half2(and_or(w, 0x00F000F0u, 0x64006400u)), s.s16, s.m72));
+}
+
+// The same values as bf16, one nibble at a time from the low four bits of each half: 128 + c, then (128 + c) s - 136 s in one
+// step, exact as well (136 s has 8 significant bits).
+__device__ __forceinline__ uint32_t nib_bf16(uint32_t w, uint32_t s2, uint32_t m136) {
+  uint32_t y;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(and_or(w, 0x000F000Fu, 0x43004300u)), "r"(s2), "r"(m136));
+  return y;
 }
 
 constexpr int WARPS = 8;
@@ -398,7 +407,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
     for (int e = 0; e < E; ++e) x[e] = 0.f;
     if (pp < n_pairs) {
       const long long off = (long long)(pp / G) * p.q_stride + (long long)(kvh * G + pp % G) * HD + lane * E;
-      if (p.q_bf16) {
+      if constexpr (!SPLIT) {
         const bf16* s = (const bf16*)p.q + off;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = __bfloat162float(s[e]);
@@ -410,7 +419,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
     }
     const RowScale rs = row_scale<E, 32>(x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = x[e] * rs.up1 * rs.up2;
+    for (int e = 0; e < E; ++e) x[e] *= rs.up;
     // element d of the row is half h of register b of lane (g = i & 7, t = d / (HD / 4)) in step 2 (word) + (n & 3) / 2, for
     // word = d % (HD / 4) / 8, n = d % 8: b = n & 1, half n / 4
 #pragma unroll
@@ -651,7 +660,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
       if (single) {
         const float inv = den == 0.f ? 0.f : 1.0f / den;
         const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
-        if (p.out_bf16) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+        if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
         else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
       } else {
         *reinterpret_cast<float4*>(p.part + (rh * parts + run) * HD + d) = a;
@@ -710,7 +719,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
       }
       const float inv = w_sm[8 * MAX_PARTS + col];
       const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
-      if (p.out_bf16) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+      if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
       else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
     }
   }
@@ -724,29 +733,27 @@ constexpr float LAZY = 5.f, MANY_BITS = 10.f;   // the maximum moves when exceed
 
 template <int HD, int NB>
 constexpr int many_smem() { return NB * TP * HD * 2 + RING * TK * HD * 2 + 2048; }
+// warps: four per block of pairs for the softmax, four for the conversion of the tiles (one block: eight, four for the keys and four
+// for the values), one per block for the multiplies
 template <int NB>
-constexpr int many_threads() { return NB * 128 + 128 + NB * 32; }
+constexpr int many_threads() { return NB * 128 + (NB == 1 ? 256 : 128) + NB * 32; }
 
 struct ManyShared {
   uint64_t full[RING], empty[RING], s_full[2][2], p_full[2][2];
   uint64_t o_done[2][2];   // by parity of the tile: a wait that skips tiles may lag one behind, never two
-  float mult[2 * TP];      // per pair: score = product x mult (log2 units)
   uint32_t tmem_base;
-  int abort, poison, max_hi;
+  uint64_t q_ready;
+  int abort, poison;
 };
 static_assert(sizeof(ManyShared) <= 2048, "fits its share of shared memory");
 
-// sixteen dims of a row as half-precision values in the order of the codes' conversion: dims 0 4 1 5 2 6 3 7 of each eight
-__device__ __forceinline__ uint4 halves8(const float* x) {
-  return make_uint4(pack_half(x[0], x[4]), pack_half(x[1], x[5]), pack_half(x[2], x[6]), pack_half(x[3], x[7]));
-}
-
-// Attention of many (row, query head) pairs of a kv head: NB blocks of 128 pairs per CTA share the key tiles, which four
-// warps convert from the cache's codes into shared memory (exact half precision, 128-byte swizzle).
-//   S = Q K^T, P = 2^10 exp2(S - m) in half precision, O += P V: tcgen05, S / P / O in tensor memory
+// Attention of many (row, query head) pairs of a kv head: NB blocks of 128 pairs per CTA share the key tiles, which warps of
+// their own convert from the cache's codes into shared memory (128-byte swizzle).
+//   S = Q K^T in bf16 (rows as they are, K exact), P = 2^10 exp2(S - m) and V in half precision, O += P V:
+//   tcgen05, S / P / O in tensor memory
 // A thread owns a pair; its maximum moves only when exceeded by 2^5 (then O is rescaled).  Scores are double-buffered: the next
-// tile's Q K^T runs under this tile's softmax.  Scaling of q, NaN blocks: as in attn_rows_kernel; where a value's NaN block was
-// met, the pairs look through the scale bytes of the keys they see once more at the end.
+// tile's Q K^T runs under this tile's softmax.  NaN blocks: as in attn_rows_kernel; where a value's NaN block was met, the pairs
+// look through the scale bytes of the keys they see once more at the end.
 template <int HD, int NB>
 __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const __grid_constant__ AttnArgs p) {
   constexpr int NH = HD / 64;                        // 64-dim halves of a row
@@ -755,6 +762,7 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = tc::smem_u32(smem);
   ManyShared* sh = reinterpret_cast<ManyShared*>(smem + NB * Q_BYTES + RING * KV_BYTES);
+  constexpr int CONV = NB == 1 ? 8 : 4, W_CONV = NB * 4, W_MMA = W_CONV + CONV;   // first warps of the roles
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int Gq = p.nq / p.nkv, Pn = p.R * Gq;
   // longest blocks first
@@ -778,52 +786,28 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
       tc::mbar_init(tc::smem_u32(&sh->p_full[s >> 1][s & 1]), 4);
       tc::mbar_init(tc::smem_u32(&sh->o_done[s >> 1][s & 1]), 1);
     }
+    tc::mbar_init(tc::smem_u32(&sh->q_ready), NB * 4);
     sh->abort = 0;
     sh->poison = 0;
-    sh->max_hi = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == NB * 4 + 4) {
+  if (warp == W_MMA) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&sh->tmem_base)), "r"(TM_COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  __syncthreads();
-  if (warp < NB * 4) {
-    // query rows: a lane takes sixteen dims, HD / 16 lanes a row
-    constexpr int LPR = HD / 16;
-#pragma unroll 1
-    for (int e = 0; e < LPR; ++e) {
-      const int qrow = (int)threadIdx.x / LPR + e * (NB * 128 / LPR), j = threadIdx.x % LPR;
-      const int pp = pair0 + qrow;
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
-      if (pp < Pn) {
-        const long long off = (long long)(pp / Gq) * p.q_stride + (long long)(kvh * Gq + pp % Gq) * HD + j * 16;
-        if (p.q_bf16) load16((const bf16*)p.q + off, x);
-        else load16((const float*)p.q + off, x);
-      }
-      const RowScale rs = row_scale<16, LPR>(x);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = x[i] * rs.up1 * rs.up2;
-      uint8_t* dst = smem + (qrow / TP) * Q_BYTES + (j >> 2) * HALF_Q + (qrow % TP) * 128;
-      const int c = (j & 3) * 2, sw = qrow & 7;
-      *reinterpret_cast<uint4*>(dst + ((c ^ sw) << 4)) = halves8(x);
-      *reinterpret_cast<uint4*>(dst + (((c + 1) ^ sw) << 4)) = halves8(x + 8);
-      if (j == 0) sh->mult[qrow] = rs.mult * rsqrtf((float)HD);
-    }
-    const int pp = pair0 + (int)threadIdx.x;
-    if (pp < Pn) atomicMax(&sh->max_hi, row_limit(p, pp / Gq));
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sh->tmem_base;
-  // key tiles of this CTA: the cache's, then the own rows'
-  const int n_cache = sh->max_hi;
+  // key tiles of this CTA: the cache's, up to the last one any of its rows sees, then the own rows'
+  int n_cache = row_limit(p, r_hi);
+  if (p.visible) {
+    n_cache = 0;
+    for (int r = r_lo + lane; r <= r_hi; r += 32) n_cache = max(n_cache, row_limit(p, r));
+    n_cache = __reduce_max_sync(0xffffffffu, n_cache);
+  }
   const int own_lo = p.own_n > 0 ? r_lo / p.T * p.T : 0;
   const int nt_c = (n_cache + TK - 1) / TK, nt_all = nt_c + (p.own_n > 0 ? (r_hi - own_lo) / TK + 1 : 0);
   const int t_lo = (int)((long long)nt_all * split / p.splits), nt = (int)((long long)nt_all * (split + 1) / p.splits) - t_lo;
@@ -840,27 +824,28 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
     return ok;
   };
 
-  if (warp >= NB * 4 && warp < NB * 4 + 4) {
-    // ---- tiles in the order the multiplies take them: K0, K1, V0, K2, V1, ...  A thread takes half a row of a tile: key
+  if (warp >= W_CONV && warp < W_MMA) {
+    // ---- tiles in the order the multiplies take them: K0, K1, V0, K2, V1, ... (tile t's keys are item 2 t - 1, its values item
+    // 2 t + 2 of the ring).  A thread takes half a row of a tile: key
     // tid % 64 (eight neighbours fill eight different 16-byte columns of the swizzle).  Codes are fetched two tiles ahead.
     constexpr int W = HD / 16;                       // words of codes per thread
-    const int tid = (int)threadIdx.x - NB * 128, row = tid & 63, part = tid >> 6;
+    const int tid = ((int)threadIdx.x - NB * 128) & 127, row = tid & 63, part = tid >> 6;
     struct Piece { uint32_t w[W], s; };
     struct Source { const uint8_t *c, *x; };         // this thread's share of key 0
     auto source = [&](const View& v, long long pos) {
       return Source{v.codes + kvh * v.head_codes + pos * (HD / 2) + part * (HD / 4),
                     v.scales + kvh * v.head_scales + pos * (HD / BLOCK) + part * (HD / 32)};
     };
-    const Source src[2][2] = {{source(p.k, 0), source(p.own_k, p.own_pos0)}, {source(p.v, 0), source(p.own_v, p.own_pos0)}};
-    auto fetch = [&](Piece& d, const Source (&sv)[2], int t) {
+    const Source kc = source(p.k, 0), ko = source(p.own_k, p.own_pos0), vc = source(p.v, 0), vo = source(p.own_v, p.own_pos0);
+    auto fetch = [&](Piece& d, bool value, int t) {
       const bool own = t_lo + t >= nt_c;
       const int key = (own ? own_lo - nt_c * TK : 0) + (t_lo + t) * TK + row, end = own ? r_hi + 1 : n_cache;
       d.s = 0;
 #pragma unroll
       for (int k = 0; k < W; ++k) d.w[k] = 0x88888888u;
       if (t < nt && key < end) {
-        const uint8_t* c = (own ? sv[1].c : sv[0].c) + (long long)key * (HD / 2);
-        const uint8_t* x = (own ? sv[1].x : sv[0].x) + (long long)key * (HD / BLOCK);
+        const uint8_t* c = (own ? (value ? vo.c : ko.c) : (value ? vc.c : kc.c)) + (long long)key * (HD / 2);
+        const uint8_t* x = (own ? (value ? vo.x : ko.x) : (value ? vc.x : kc.x)) + (long long)key * (HD / BLOCK);
 #pragma unroll
         for (int k = 0; k < W / 4; ++k) {
           const uint4 u = __ldg(reinterpret_cast<const uint4*>(c) + k);
@@ -870,11 +855,11 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
         else d.s = __ldg(reinterpret_cast<const unsigned short*>(x));
       }
     };
-    uint32_t slot = 0, phase = 1;                    // (the first pass finds every slot free)
     const uint32_t dst0 = base + NB * Q_BYTES + (HD == 128 ? part * HALF_KV : 0) + row * 128;
     const uint32_t col0 = (uint32_t)((row & 7) << 4) ^ (HD == 128 ? 0u : (uint32_t)part * 64u);
-    auto convert = [&](Piece& d, bool value) {
-      if (!warp_wait(&sh->empty[slot], phase)) return;
+    auto convert = [&](Piece& d, bool value, uint32_t item) {
+      const uint32_t slot = item % RING;
+      if (!warp_wait(&sh->empty[slot], ((item / RING) & 1u) ^ 1u)) return;   // (the first pass finds every slot free)
       if (value && __vcmpeq4(d.s, 0xffffffffu)) {
         sh->poison = 1;
 #pragma unroll
@@ -882,47 +867,75 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
           if (((d.s >> (8 * k)) & 255u) == NAN_SCALE) d.s &= ~(255u << (8 * k));
       }
       const uint32_t dst = dst0 + slot * KV_BYTES;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        const uint32_t sb = (d.s >> (8 * (k >> 1))) & 255u;
-        const Scale2 sc = scale2(sb, sb);
-        const uint32_t w = d.w[k], w8 = w >> 8;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (col0 ^ (uint32_t)(k << 4))), "r"(nib_lo(w, sc)),
-                     "r"(nib_hi(w, sc)), "r"(nib_lo(w8, sc)), "r"(nib_hi(w8, sc))
+      auto put = [&](int k, uint32_t a, uint32_t b, uint32_t c, uint32_t e) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (col0 ^ (uint32_t)(k << 4))), "r"(a), "r"(b), "r"(c), "r"(e)
                      : "memory");
+      };
+      if (value) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          const uint32_t sb = (d.s >> (8 * (k >> 1))) & 255u;
+          const Scale2 sc = scale2(sb, sb);
+          const uint32_t w = d.w[k], w8 = w >> 8;
+          put(k, nib_lo(w, sc), nib_hi(w, sc), nib_lo(w8, sc), nib_hi(w8, sc));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          const float f = scale_of((d.s >> (8 * (k >> 1))) & 255u);
+          const uint32_t sc = pack_bf16(f, f), off = pack_bf16(f * -136.f, f * -136.f), w = d.w[k];
+          put(k, nib_bf16(w, sc, off), nib_bf16(w >> 4, sc, off), nib_bf16(w >> 8, sc, off), nib_bf16(w >> 12, sc, off));
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->full[slot])) : "memory");
-      if (++slot == RING) { slot = 0; phase ^= 1u; }
     };
-    Piece dk[3], dv[3];
-    if (nt > 0) {
-      fetch(dk[0], src[0], 0);
-      fetch(dk[1], src[0], 1);
-      fetch(dv[0], src[1], 0);
-      fetch(dk[2], src[0], 2);
-      fetch(dv[1], src[1], 1);
-      convert(dk[0], false);
-    }
-#pragma unroll 1
-    for (int t = 0; t < nt && ok; t += 3) {
+    if constexpr (NB == 1) {
+      // one block: its softmax takes a tile faster than four warps convert one, so four take the keys and four the values
+      const bool value = warp >= W_CONV + 4;
+      Piece d[3];
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        if (t + k < nt && ok) {
-          fetch(dk[k], src[0], t + k + 3);
-          fetch(dv[(k + 2) % 3], src[1], t + k + 2);
-          if (t + k + 1 < nt) convert(dk[(k + 1) % 3], false);
-          if (ok) convert(dv[k], true);
+      for (int k = 0; k < 3; ++k) fetch(d[k], value, k);
+#pragma unroll 1
+      for (int t = 0; t < nt && ok; t += 3) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          if (t + k < nt && ok) {
+            convert(d[k], value, value ? 2 * (t + k) + 2 : max(2 * (t + k) - 1, 0));
+            fetch(d[k], value, t + k + 3);
+          }
+        }
+      }
+    } else {
+      Piece dk[3], dv[3];
+      if (nt > 0) {
+        fetch(dk[0], false, 0);
+        fetch(dk[1], false, 1);
+        fetch(dv[0], true, 0);
+        fetch(dk[2], false, 2);
+        fetch(dv[1], true, 1);
+        convert(dk[0], false, 0);
+      }
+#pragma unroll 1
+      for (int t = 0; t < nt && ok; t += 3) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          if (t + k < nt && ok) {
+            fetch(dk[k], false, t + k + 3);
+            fetch(dv[(k + 2) % 3], true, t + k + 2);
+            if (t + k + 1 < nt) convert(dk[(k + 1) % 3], false, 2 * (t + k) + 1);
+            if (ok) convert(dv[k], true, 2 * (t + k) + 2);
+          }
         }
       }
     }
     if (!ok) sh->abort = 1;
-  } else if (warp >= NB * 4 + 4) {
+  } else if (warp >= W_MMA) {
     // ---- multiplies: a warp per block of pairs, so that one's waits are covered by the other's multiplies (one warp for both:
-    // 2350 cycles per tile of 2 x 128 pairs, of which the tensor pipe worked 1280).  Both operands half precision, fp32 accumulators.
-    const int bl = warp - (NB * 4 + 4);
-    const uint32_t idesc_qk = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
+    // 2350 cycles per tile of 2 x 128 pairs, of which the tensor pipe worked 1280).  Q K^T takes bf16, P V half precision.
+    const int bl = warp - W_MMA;
+    const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TK >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
     const uint32_t idesc_pv = (1u << 4) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(TP >> 4) << 24);
     const uint32_t el = wide::elect_one();
     const uint32_t t_s = tmem + bl * 128, t_o = tmem + O_COL + bl * 128;
@@ -944,9 +957,10 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
       wide::commit_one(tc::smem_u32(&sh->empty[slot]), el);
       next();
     };
-    if (nt > 0) scores(0);
+    if (nt > 0 && warp_wait(&sh->q_ready, 0)) scores(0);
     for (int t = 0; t < nt && ok; ++t) {
-      if (t + 1 < nt) scores(t + 1);   // (buffer of tile t - 1: its P V was issued before, the tensor pipe keeps the order)
+      if (t + 1 == nt) next();         // (no item 2 nt - 1)
+      else scores(t + 1);              // (buffer of tile t - 1: its P V was issued before, the tensor pipe keeps the order)
       if (!ok || !warp_wait(&sh->full[slot], phase) || !warp_wait(&sh->p_full[bl][t & 1], (t >> 1) & 1u)) break;
       // V tile: key rows of 64 dims, the MN-major form of B (64-dim halves HALF_KV apart)
       const uint64_t db = (tc::make_smem_desc(base + NB * Q_BYTES + slot * KV_BYTES) & ~(0x3FFFull << 16)) |
@@ -960,19 +974,60 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
     }
     if (!ok) sh->abort = 1;
   } else {
+    // ---- query rows: a lane takes sixteen dims, HD / 16 lanes a row
+    {
+      constexpr int LPR = HD / 16, STEP_ROWS = NB * 128 / LPR;
+      const int j = threadIdx.x % LPR;
+      int qrow = (int)threadIdx.x / LPR, rr = (pair0 + qrow) / Gq, hh = (pair0 + qrow) - rr * Gq;
+      const int dr = STEP_ROWS / Gq, dh = STEP_ROWS - dr * Gq;
+#pragma unroll 1
+      for (int e0 = 0; e0 < LPR; e0 += 4) {   // four rows' loads are in flight at a time
+        uint4 w[4][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e][0] = w[e][1] = make_uint4(0, 0, 0, 0);
+          if (rr < p.R) {
+            const uint4* src = reinterpret_cast<const uint4*>((const bf16*)p.q + (long long)rr * p.q_stride +
+                                                              (long long)(kvh * Gq + hh) * HD + j * 16);
+            w[e][0] = src[0];
+            w[e][1] = src[1];
+          }
+          rr += dr;
+          hh += dh;
+          if (hh >= Gq) { hh -= Gq; ++rr; }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e, qrow += STEP_ROWS) {
+          uint8_t* dst = smem + (qrow / TP) * Q_BYTES + (j >> 2) * HALF_Q + (qrow % TP) * 128;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {       // the order of the codes' conversion: dims 0 4, 1 5, 2 6, 3 7 of each eight
+            const uint4 u = w[e][h];
+            *reinterpret_cast<uint4*>(dst + ((((j & 3) * 2 + h) ^ (qrow & 7)) << 4)) =
+                make_uint4(__byte_perm(u.x, u.z, 0x5410), __byte_perm(u.x, u.z, 0x7632), __byte_perm(u.y, u.w, 0x5410),
+                           __byte_perm(u.y, u.w, 0x7632));
+          }
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(&sh->q_ready)) : "memory");
+    }
     // ---- softmax: a thread per pair
     const int bl = warp >> 2, pp = pair0 + (int)threadIdx.x;
     const bool pv = pp < Pn;
     const int r = pv ? pp / Gq : 0, hq = kvh * Gq + (pv ? pp % Gq : 0);
     const int own_first = r / p.T * p.T, lim = pv ? row_limit(p, r) : 0;
-    const float mult = lim > 0 || p.own_n > 0 ? sh->mult[threadIdx.x] : 1.f;   // (a row that sees nothing: zeros whatever its query)
+    const float scale = 1.4426950408889634f * rsqrtf((float)HD);   // scores in units of log2
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + bl * 128;
     const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + O_COL + bl * 128;
+    // tiles that all of the warp's pairs see whole
+    const int whole = min(nt_c, __reduce_min_sync(0xffffffffu, pv ? lim : 0x7fffffff) / TK) - t_lo;
+    bool seen = min(whole, nt) > 0;  // the pair sees some key of this part
     float m = -INFINITY, l = 0.f;
-    for (int t = 0; t < nt; ++t) {
+    for (int t = 0; t < nt && ok; ++t) {
       if (!warp_wait(&sh->s_full[bl][t & 1], (t >> 1) & 1u)) break;
-      float s[TK];
       const uint32_t t_s = t_row + (t & 1) * TK;
+      float s[TK];
       {
         float a[32], c[32];
         wide::tmem_ld<32>(t_s, a);
@@ -981,32 +1036,33 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
 #pragma unroll
         for (int k = 0; k < 32; ++k) { s[k] = a[k]; s[32 + k] = c[k]; }
       }
-      // visible keys of the tile: [lo, hi)
-      const int tt = t_lo + t;
-      int lo = 0, hi = TK;
-      if (tt < nt_c) {
-        hi = min(TK, lim - tt * TK);
-      } else {
-        const int y = own_lo + (tt - nt_c) * TK;
-        lo = max(0, own_first - y);
-        hi = min(TK, r + 1 - y);
-      }
-      if (!pv) { lo = 0; hi = TK; }   // (nothing of these pairs is stored)
-      if (__any_sync(0xffffffffu, hi < TK)) {
+      if (t >= whole) {   // visible keys of the tile: [lo, hi)
+        const int tt = t_lo + t;
+        int lo = 0, hi = TK;
+        if (tt < nt_c) {
+          hi = lim - tt * TK;
+        } else {
+          const int y = own_lo + (tt - nt_c) * TK;
+          lo = own_first - y;
+          hi = r + 1 - y;
+        }
+        if (!pv) { lo = 0; hi = TK; }   // (nothing of these pairs is stored)
+        seen |= min(hi, TK) > max(lo, 0);
+        if (__any_sync(0xffffffffu, hi < TK)) {
 #pragma unroll
-        for (int k = 0; k < TK; ++k)
-          if (k >= hi) s[k] = -INFINITY;
-      }
-      if (__any_sync(0xffffffffu, lo > 0)) {
+          for (int k = 0; k < TK; ++k)
+            if (k >= hi) s[k] = -INFINITY;
+        }
+        if (__any_sync(0xffffffffu, lo > 0)) {
 #pragma unroll
-        for (int k = 0; k < TK; ++k)
-          if (k < lo) s[k] = -INFINITY;
+          for (int k = 0; k < TK; ++k)
+            if (k < lo) s[k] = -INFINITY;
+        }
       }
       float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
       for (int k = 0; k < TK; k += 2) m4[(k >> 1) & 3] = max3(m4[(k >> 1) & 3], s[k], s[k + 1]);
-      float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-      mx = mx == -INFINITY ? mx : mx * mult;          // (no visible key: -inf whatever the factor)
+      const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale;
       const bool grow = t > 0 && mx > m + LAZY;       // (also the first visible key of the row: m = -inf)
       if (t == 0) {
         m = mx;
@@ -1028,12 +1084,12 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       }
       const float mm = m == -INFINITY ? 0.f : m - MANY_BITS;   // no visible key so far: all weights are exp2(-inf) = 0
-      const float2 mult2 = make_float2(mult, mult), off2 = make_float2(-mm, -mm);
+      const float2 scale2v = make_float2(scale, scale), off2 = make_float2(-mm, -mm);
       float2 r2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       uint32_t ph[32];
 #pragma unroll
       for (int k = 0; k < TK; k += 2) {
-        const float2 x = fma2(make_float2(s[k], s[k + 1]), mult2, off2);
+        const float2 x = fma2(make_float2(s[k], s[k + 1]), scale2v, off2);
         const float2 e = make_float2(ex2(x.x), ex2(x.y));
         r2[(k >> 1) & 1] = add2(r2[(k >> 1) & 1], e);
         ph[k >> 1] = pack_half(e.x, e.y);
@@ -1048,6 +1104,8 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
     if (ok && nt > 0) warp_wait(&sh->o_done[bl][(nt - 1) & 1], ((nt - 1) >> 1) & 1u);
     if (!ok) sh->abort = 1;
     if (ok) {
+      // scores of minus infinity alone: a query with an infinity in it
+      if (seen && l == 0.f) l = __int_as_float(0x7fffffff);
       // (poison was written before the last tile's barrier; NaN blocks among the keys this pair sees)
       uint32_t bad = 0;
       if (*(volatile int*)&sh->poison && pv) {
@@ -1065,7 +1123,11 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
       }
       const bool part = p.splits > 1;
       const float inv = part ? 1.f : (l == 0.f ? 0.f : 1.0f / l);
-      const long long idx = ((long long)r * p.nq + hq) * p.splits + split;
+      // part: [item, split][dim][pair], neighbouring lanes side by side
+      float* dst_part = p.part + (long long)blockIdx.x * HD * (NB * TP) + threadIdx.x;
+      // out: a warp's 32 rows through shared memory (the queries' place: every multiply is done), so that whole rows go out
+      constexpr int CPR = HD / 8;      // 16-byte pieces of a row
+      uint8_t* stage = smem + warp * 32 * HD * 2;
 #pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
         float o[32];
@@ -1082,18 +1144,31 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
           const int dim = (k & ~7) + ((k & 1) << 2) + ((k & 7) >> 1);   // columns hold dims 0 4 1 5 2 6 3 7 of each eight
           f[dim] = ((bad >> ((c + k) >> 4)) & 1u) ? __int_as_float(0x7fffffff) : o[k] * inv;
         }
-        if (!part) {
-          bf16* dst = (bf16*)p.out + (long long)r * p.out_stride + (long long)hq * HD + c;
+        if (part) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            wide::st16b(dst + 8 * k, pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]),
-                        pack_bf16(f[8 * k + 4], f[8 * k + 5]), pack_bf16(f[8 * k + 6], f[8 * k + 7]), pv);
+          for (int k = 0; k < 32; ++k) dst_part[(c + k) * (NB * TP)] = f[k];
         } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) wide::st8(p.part + idx * HD + c + 8 * k, f + 8 * k, true, pv);
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<uint4*>(stage + lane * HD * 2 + (((c / 8 + k) ^ (lane & (CPR - 1))) << 4)) =
+                make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]),
+                           pack_bf16(f[8 * k + 4], f[8 * k + 5]), pack_bf16(f[8 * k + 6], f[8 * k + 7]));
         }
       }
-      if (pv && part) p.part_ml[idx] = make_float2(m, l);
+      if (part) {
+        p.part_ml[(long long)blockIdx.x * (NB * TP) + threadIdx.x] = make_float2(m, l);
+      } else {
+        __syncwarp();
+        const long long mine = pv ? (long long)r * p.out_stride + (long long)hq * HD : -1;
+        const int col = lane & (CPR - 1);
+#pragma unroll 4
+        for (int i = 0; i < 32; i += 32 / CPR) {
+          const int row = i + lane / CPR;
+          const long long off = __shfl_sync(0xffffffffu, mine, row);
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + row * HD * 2 + ((col ^ (row & (CPR - 1))) << 4));
+          if (off >= 0) *reinterpret_cast<uint4*>((bf16*)p.out + off + col * 8) = v;
+        }
+      }
     }
   }
 
@@ -1101,43 +1176,57 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
   __syncthreads();
   if (sh->abort)
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-  if (warp == NB * 4 + 4) {
+  if (warp == W_MMA) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TM_COLS) : "memory");
   }
 }
 
-// The parts of a (row, query head), in their order: a warp each.
-template <int HD>
+// The parts of each pair of attn_many_kernel, in their order.  A thread takes four dims of a pair; neighbouring threads
+// neighbouring pairs, as the parts lie.  Sixteen parts' loads are in flight at a time.
+template <int HD, int NB>
 __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ AttnArgs p) {
-  const long long rh = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (rh >= (long long)p.R * p.nq) return;
-  const int lane = threadIdx.x & 31, parts = p.splits;
-  constexpr int E = HD / 32;
-  const float2* ml = p.part_ml + rh * parts;
-  float mx = -INFINITY;
-  for (int i = 0; i < parts; ++i) mx = fmaxf(mx, __ldcg(&ml[i]).x);
-  float den = 0.f, a[E];
+  constexpr int PAIRS = NB * TP, CHUNKS = 256 / PAIRS, PER = HD / 4 / CHUNKS;   // pieces of four dims per CTA, CTAs per item
+  const int item = blockIdx.x / PER, chunk = blockIdx.x % PER * CHUNKS + (int)threadIdx.x / PAIRS;
+  const int pair = threadIdx.x % PAIRS, Gq = p.nq / p.nkv;
+  const int kvh = item % p.nkv, pp = (p.blocks - 1 - item / p.nkv) * PAIRS + pair;
+  if (pp >= p.R * Gq) return;
+  const float2* ml = p.part_ml + (long long)item * p.splits * PAIRS + pair;
+  const float* src = p.part + ((long long)item * p.splits * HD + chunk * 4) * PAIRS + pair;
+  float mx = -INFINITY, den = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int i0 = 0; i0 < p.splits; i0 += 16) {
+    float2 v[16];
+    float x[16][4];
 #pragma unroll
-  for (int e = 0; e < E; ++e) a[e] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    const float2 v = __ldcg(&ml[i]);
-    const float w = v.x == -INFINITY ? (v.y == 0.f ? 0.f : 1.f) : exp2f(v.x - mx);   // (a sum without a maximum is 0, or NaN)
-    den = fmaf(v.y, w, den);
-    const float* src = p.part + (rh * parts + i) * HD + lane * E;
-    if constexpr (E == 4) {
-      const float4 u = __ldcg(reinterpret_cast<const float4*>(src));
-      a[0] = fmaf(w, u.x, a[0]); a[1] = fmaf(w, u.y, a[1]); a[2] = fmaf(w, u.z, a[2]); a[3] = fmaf(w, u.w, a[3]);
-    } else {
-      const float2 u = __ldcg(reinterpret_cast<const float2*>(src));
-      a[0] = fmaf(w, u.x, a[0]); a[1] = fmaf(w, u.y, a[1]);
+    for (int i = 0; i < 16; ++i) {
+      v[i] = make_float2(-INFINITY, 0.f);
+      if (i0 + i < p.splits) v[i] = __ldcg(ml + (i0 + i) * PAIRS);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] = i0 + i < p.splits ? __ldcg(src + ((long long)(i0 + i) * HD + e) * PAIRS) : 0.f;
+    float m2 = mx;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m2 = fmaxf(m2, v[i].x);
+    const float corr = mx == -INFINITY ? 1.f : exp2f(mx - m2);      // (nothing so far, or sums without a maximum: NaN)
+    den *= corr;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] *= corr;
+    mx = m2;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float w = v[i].x == -INFINITY ? (v[i].y == v[i].y ? 0.f : 1.f) : exp2f(v[i].x - mx);
+      den = fmaf(v[i].y, w, den);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] = fmaf(w, x[i][e], a[e]);
     }
   }
   const float inv = den == 0.f ? 0.f : 1.0f / den;
-  bf16* dst = (bf16*)p.out + rh / p.nq * p.out_stride + rh % p.nq * HD + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; e += 2) reinterpret_cast<uint32_t*>(dst)[e >> 1] = pack_bf16(a[e] * inv, a[e + 1] * inv);
+  const int r = pp / Gq;
+  *reinterpret_cast<uint2*>((bf16*)p.out + (long long)r * p.out_stride + (long long)(kvh * Gq + pp - r * Gq) * HD + chunk * 4) =
+      make_uint2(pack_bf16(a[0] * inv, a[1] * inv), pack_bf16(a[2] * inv, a[3] * inv));
 }
 
 }  // namespace kv4
