@@ -121,10 +121,10 @@ bool config_ok(const clasp_config* c) {
 bool is_kv4(const clasp_config& c) { return (c.flags & CLASP_FLAG_KV4) != 0; }
 
 // Keys per run of the attention over a 4-bit cache.  A function of the capacity and the kv heads alone, so that verification
-// and one-token decoding sum a position's keys in the same order; at full capacity two CTAs per SM have a run.
+// and one-token decoding sum a position's keys in the same order; at full capacity nearly every SM has a run.
 int kv4_run_len(const clasp_config& c) {
   const int step = clasp::kv4::WARPS * clasp::kv4::STEP;
-  const int target = std::max(1, std::min(clasp::kv4::MAX_PARTS - 4, 2 * 148 / c.n_kv_heads));
+  const int target = std::max(1, std::min(clasp::kv4::MAX_PARTS - 4, 148 / c.n_kv_heads));
   return std::max(1, ((c.max_ctx + target - 1) / target + step - 1) / step) * step;
 }
 int kv4_max_parts(const clasp_config& c) {
@@ -217,7 +217,11 @@ cudaError_t kv4_attributes() {
   namespace k4 = clasp::kv4;
   const struct { const void* f; int bytes; } k[] = {
       {(const void*)k4::attn_many_kernel<128, 1>, k4::many_smem<128, 1>()}, {(const void*)k4::attn_many_kernel<128, 2>, k4::many_smem<128, 2>()},
-      {(const void*)k4::attn_many_kernel<64, 1>, k4::many_smem<64, 1>()}, {(const void*)k4::attn_many_kernel<64, 2>, k4::many_smem<64, 2>()}};
+      {(const void*)k4::attn_many_kernel<64, 1>, k4::many_smem<64, 1>()}, {(const void*)k4::attn_many_kernel<64, 2>, k4::many_smem<64, 2>()},
+      {(const void*)k4::attn_rows_kernel<128, 1, false>, k4::rows_smem<128, 1, false>()}, {(const void*)k4::attn_rows_kernel<128, 2, false>, k4::rows_smem<128, 2, false>()},
+      {(const void*)k4::attn_rows_kernel<128, 1, true>, k4::rows_smem<128, 1, true>()}, {(const void*)k4::attn_rows_kernel<128, 2, true>, k4::rows_smem<128, 2, true>()},
+      {(const void*)k4::attn_rows_kernel<64, 1, false>, k4::rows_smem<64, 1, false>()}, {(const void*)k4::attn_rows_kernel<64, 2, false>, k4::rows_smem<64, 2, false>()},
+      {(const void*)k4::attn_rows_kernel<64, 1, true>, k4::rows_smem<64, 1, true>()}, {(const void*)k4::attn_rows_kernel<64, 2, true>, k4::rows_smem<64, 2, true>()}};
   for (const auto& e : k) {
     const cudaError_t rc = cudaFuncSetAttribute(e.f, cudaFuncAttributeMaxDynamicSharedMemorySize, e.bytes);
     if (rc != cudaSuccess) return rc;
@@ -608,13 +612,12 @@ template <int HD, bool SPLIT>
 int kv4_rows_launch(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
   namespace k4 = clasp::kv4;
   const int pairs = p.R * (p.nq / p.nkv);
-  // pairs per CTA: the fewest that hold them all, since every block of pairs reads the run again (SPLIT: the second operands
-  // take the registers of a third and fourth group)
-  const int nt = pairs <= 8 ? 1 : (pairs <= 16 || SPLIT) ? 2 : 4;
+  // eight or sixteen pairs per CTA (a block of pairs reads the run again: at sixteen the multiplies weigh as much as the
+  // conversion, and 24 or 32 would need more registers than sixteen warps leave)
+  const int nt = pairs <= 8 ? 1 : 2;
   const dim3 grid(p.runs + (p.own_n > 0 ? 1 : 0), p.nkv, (pairs + 8 * nt - 1) / (8 * nt));
-  if (nt == 1) k4::attn_rows_kernel<HD, 1, SPLIT><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
-  else if (nt == 2) k4::attn_rows_kernel<HD, 2, SPLIT><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
-  else if constexpr (!SPLIT) k4::attn_rows_kernel<HD, 4, false><<<grid, k4::WARPS * 32, 0, ctx->stream>>>(p);
+  if (nt == 1) k4::attn_rows_kernel<HD, 1, SPLIT><<<grid, k4::WARPS * 32, k4::rows_smem<HD, 1, SPLIT>(), ctx->stream>>>(p);
+  else k4::attn_rows_kernel<HD, 2, SPLIT><<<grid, k4::WARPS * 32, k4::rows_smem<HD, 2, SPLIT>(), ctx->stream>>>(p);
   return launch_check(ctx);
 }
 
@@ -1441,8 +1444,7 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
         cudaFuncSetAttribute(clasp::wide::gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, clasp::wide::GEMM_SMEM) !=
             cudaSuccess ||
         cudaFuncSetAttribute(clasp::wide::attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, clasp::wide::ATT_SMEM) !=
-            cudaSuccess ||
-        kv4_attributes() != cudaSuccess) {
+            cudaSuccess) {
       delete ctx;
       return CLASP_ERR_CUDA;
     }
@@ -1454,7 +1456,7 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
     delete ctx;
     return CLASP_ERR_CUDA;
   }
-  if (s32_setup(ctx) != CLASP_OK) {
+  if (s32_setup(ctx) != CLASP_OK || (is_kv4(*cfg) && kv4_attributes() != cudaSuccess)) {
     delete ctx;
     return CLASP_ERR_CUDA;
   }

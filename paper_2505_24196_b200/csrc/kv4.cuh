@@ -334,8 +334,9 @@ __device__ __forceinline__ uint32_t nib_bf16(uint32_t w, uint32_t s2, uint32_t m
   return y;
 }
 
-constexpr int WARPS = 8;
+constexpr int WARPS = 16;
 constexpr int STEP = 16;                 // keys a warp takes at a time
+constexpr int STAGES = 4;                // steps of a warp in shared memory: one at work, three on their way
 constexpr int MAX_PARTS = 152;           // runs of one launch and the own rows
 constexpr float P_BITS = 12.f;           // weights are held as 2^12 .. 2^20 x exp2(s - m) in half precision (see below)
 
@@ -343,16 +344,26 @@ template <int HD> struct Raw {           // one warp step: two key rows' and fou
   uint32_t k[2][HD / 32], v[4][HD / 64];
   uint32_t ks[2], vs;
 };
+template <int HD> constexpr int STEP_BYTES = STEP * (HD + HD / 8);
+template <int HD, int NT, bool SPLIT> constexpr int rows_smem() {
+  constexpr int ring = WARPS * STAGES * STEP_BYTES<HD>, merge = WARPS * 8 * (HD + 4) * 4;
+  return (ring > merge ? ring : merge) + (SPLIT ? 2 : 1) * NT * (HD / 16) * 32 * 8;
+}
+template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool in) {
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16u : 0u) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(in ? (uint32_t)N : 0u), "n"(N) : "memory");
+}
 
 // Attention of few (row, query head) pairs: 8 NT pairs of one kv head per CTA, one run of the cache per CTA, its steps of 16
-// keys dealt to eight warps that never wait for one another before the end.
+// keys dealt to sixteen warps that never wait for one another before the end.
 //
 //   S^T = K q^T     16 keys x 8 pairs: the keys are the M rows of mma.m16n8k16, so few pairs waste little
 //   O^T = V^T P^T   16 dims x 8 pairs
 //
-// Which key an M row is and which dim a k index is, is free as long as both operands agree, so every lane gets its pieces of
-// K and V by 16- and 8-byte loads straight from the cache (no shared memory) and converts them in place: lane (g, t) of a
-// step holds dims [32 t, 32 t + 32) of two keys, and 16 dims [16 g, 16 g + 16) of four values (hd 128).  K and V are exact in
+// Which key an M row is and which dim a k index is, is free as long as both operands agree, so a lane gets its pieces of
+// K and V in 16- and 8-byte loads and converts them in place: lane (g, t) of a step holds dims [32 t, 32 t + 32) of two keys, and
+// 16 dims [16 g, 16 g + 16) of four values (hd 128).  A warp copies its steps to a ring of its own, three ahead (asynchronous
+// copies: the bytes on their way cost no registers), with the rows placed so that those loads meet no bank twice.  K and V are exact in
 // half precision.  q is scaled by a power of two per row to a largest magnitude in [2^13, 2^14) and rounded to half precision:
 // exact for bf16 rows (what lies 2^24 below the row's maximum aside); SPLIT (fp32 models) adds the rounding error of q and of
 // the weights as a second half-precision operand: 22 bits.  Weights: half precision of 2^12 exp2(s - m), m a maximum that moves
@@ -360,19 +371,20 @@ template <int HD> struct Raw {           // one warp step: two key rows' and fou
 // A block with the NaN byte must reach only the rows that see it, and 0 x NaN is NaN: values' NaN blocks enter as zeros, and
 // `poison` remembers which (pair, block) they belong to.
 template <int HD, int NT, bool SPLIT>
-__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(const __grid_constant__ AttnArgs p) {
+__global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_constant__ AttnArgs p) {
   constexpr int PB = 8 * NT;             // pairs per CTA
   constexpr int KS = HD / 16;            // k steps of the scores, and tiles of 16 dims of the output
   constexpr int KW = HD / 32, VW = HD / 64;
   constexpr int PARTS = SPLIT ? 2 : 1;
   constexpr float NEG = -INFINITY;
-  __shared__ uint2 qf[PARTS][NT][KS][32];
-  __shared__ float o_sm[WARPS][8][HD + 4];
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint2 (*qf)[NT][KS][32] = reinterpret_cast<uint2 (*)[NT][KS][32]>(smem);
+  uint8_t* ring = smem + PARTS * NT * KS * 32 * 8;                       // the warps' steps, later their results
+  float (*o_sm)[8][HD + 4] = reinterpret_cast<float (*)[8][HD + 4]>(ring);
   __shared__ float2 ml_sm[WARPS][PB];
   __shared__ float mult_sm[PB];
   __shared__ int lo_sm[PB], hi_sm[PB];
   __shared__ uint32_t poison_sm[8];
-  __shared__ int range_sm[4];            // largest lo, smallest hi, smallest lo, largest hi
   __shared__ int last_sm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int run = blockIdx.x, kvh = blockIdx.y, pb = blockIdx.z;
@@ -380,24 +392,94 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
   const bool own = run >= p.runs;
   const int pair0 = pb * PB;
 
-  if (threadIdx.x < 8) poison_sm[threadIdx.x] = 0;
-  if (threadIdx.x == 8) { range_sm[0] = 0; range_sm[1] = 0x7fffffff; range_sm[2] = 0x7fffffff; range_sm[3] = 0; }
-  __syncthreads();
-  if (threadIdx.x < PB) {
-    const int pp = pair0 + (int)threadIdx.x;
-    int lo = 0, hi = 0;
-    if (pp < n_pairs) {
-      const int r = pp / G;
-      if (own) { lo = (p.r0 + r) / p.T * p.T; hi = p.r0 + r + 1; }
-      else hi = row_limit(p, r);
-      atomicMax(&range_sm[0], lo);
-      atomicMin(&range_sm[1], hi);
-      atomicMin(&range_sm[2], lo);
-      atomicMax(&range_sm[3], hi);
-    }
-    lo_sm[threadIdx.x] = lo;
-    hi_sm[threadIdx.x] = hi;
+  // what each pair sees (every warp for itself; the masks read it from shared memory)
+  int lo = 0, hi = 0;
+  const bool mine = lane < PB && pair0 + lane < n_pairs;
+  if (mine) {
+    const int r = (pair0 + lane) / G;
+    if (own) { lo = (p.r0 + r) / p.T * p.T; hi = p.r0 + r + 1; }
+    else hi = row_limit(p, r);
   }
+  if (warp == 0 && lane < PB) { lo_sm[lane] = lo; hi_sm[lane] = hi; }
+  if (threadIdx.x < 8) poison_sm[threadIdx.x] = 0;
+  const int first = __reduce_min_sync(0xffffffffu, mine ? lo : 0x7fffffff), last = __reduce_max_sync(0xffffffffu, hi);
+  // keys of this CTA
+  int k_lo, k_end;
+  if (own) {
+    k_lo = first;
+    k_end = min(last, p.own_n);
+  } else {
+    k_lo = run * p.run_len;
+    k_end = min(min(k_lo + p.run_len, p.n_keys), last);
+  }
+  const int full_lo = __reduce_max_sync(0xffffffffu, lo);
+  const int full_hi = min(__reduce_min_sync(0xffffffffu, mine ? hi : 0x7fffffff), k_end);
+  const long long pos_off = own ? p.own_pos0 : 0;
+  const View& vk = own ? p.own_k : p.k;
+  const View& vv = own ? p.own_v : p.v;
+  const uint8_t* kc = vk.codes + kvh * vk.head_codes + pos_off * (HD / 2);
+  const uint8_t* kx = vk.scales + kvh * vk.head_scales + pos_off * (HD / BLOCK);
+  const uint8_t* vc = vv.codes + kvh * vv.head_codes + pos_off * (HD / 2);
+  const uint8_t* vx = vv.scales + kvh * vv.head_scales + pos_off * (HD / BLOCK);
+  const int kg = (g >> 1) + 4 * (g & 1);   // key of M row g; row g + 8 is key kg + 8
+  // A step in shared memory: K codes, V codes, K scales, V scales.  Key k's row of K lies where M row g = k is (so that g's rows
+  // follow one another); of V, the 16-byte pieces of keys 2, 3 of each four are swapped in pairs (hd 128).
+  constexpr int ROW = HD / 2, KV_STEP = STEP * ROW, SC = HD / BLOCK;
+  const uint32_t my_ring = tc::smem_u32(ring) + warp * STAGES * STEP_BYTES<HD>;
+  auto fetch = [&](int stage, int base) {
+    const uint32_t dst = my_ring + stage * STEP_BYTES<HD>;
+#pragma unroll
+    for (int i = 0; i < ROW / 32; ++i) {
+      const int c = lane + 32 * i, key = c / (ROW / 16), piece = c % (ROW / 16);
+      const bool in = base + key < k_end;
+      const long long off = (long long)(in ? base + key : k_lo) * ROW + piece * 16;
+      const int slot = (key & 8) + ((key & 3) << 1) + ((key >> 2) & 1);
+      cp_async<16>(dst + slot * ROW + piece * 16, kc + off, in);
+      cp_async<16>(dst + KV_STEP + key * ROW + (HD == 128 ? piece ^ (key & 2) : piece) * 16, vc + off, in);
+    }
+    const int key = lane & 15;
+    const bool in = base + key < k_end;
+    cp_async<SC>(dst + 2 * KV_STEP + (lane >> 4) * STEP * SC + key * SC,
+                 (lane < 16 ? kx : vx) + (long long)(in ? base + key : k_lo) * SC, in);
+  };
+  auto take = [&](Raw<HD>& w, int stage) {
+    const uint8_t* s = ring + (warp * STAGES + stage) * STEP_BYTES<HD>;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint8_t* a = s + (g + 8 * i) * ROW + t * (HD / 8);
+      const uint8_t* x = s + 2 * KV_STEP + (kg + 8 * i) * SC + t * (HD / 64);
+      if constexpr (HD == 128) {
+        const uint4 u = *reinterpret_cast<const uint4*>(a);
+        w.k[i][0] = u.x; w.k[i][1] = u.y; w.k[i][2] = u.z; w.k[i][3] = u.w;
+        w.ks[i] = *reinterpret_cast<const unsigned short*>(x);
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(a);
+        w.k[i][0] = u.x; w.k[i][1] = u.y;
+        w.ks[i] = *x;
+      }
+    }
+    w.vs = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = t + 4 * i;
+      const uint8_t* a = s + KV_STEP + key * ROW;
+      if constexpr (HD == 128) {
+        const uint2 u = *reinterpret_cast<const uint2*>(a + (((g >> 1) ^ (t & 2)) << 4) + ((g & 1) << 3));
+        w.v[i][0] = u.x; w.v[i][1] = u.y;
+      } else {
+        w.v[i][0] = *reinterpret_cast<const uint32_t*>(a + g * 4);
+      }
+      w.vs |= (uint32_t)s[2 * KV_STEP + STEP * SC + key * SC + (HD == 128 ? g : g >> 1)] << (8 * i);
+    }
+  };
+
+  int base = k_lo + warp * STEP, stage = 0;
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) {
+    if (base + i * WARPS * STEP < k_end) fetch(i, base + i * WARPS * STEP);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+
   // q rows into the fragments of the second operand: a warp per pair, lane = its place along the row
   for (int i = warp; i < PB; i += WARPS) {
     const int pp = pair0 + i;
@@ -438,55 +520,6 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
   }
   __syncthreads();
 
-  // keys of this CTA
-  int k_lo, k_end;
-  if (own) {
-    k_lo = range_sm[2];
-    k_end = min(range_sm[3], p.own_n);
-  } else {
-    k_lo = run * p.run_len;
-    k_end = min(min(k_lo + p.run_len, p.n_keys), range_sm[3]);
-  }
-  const int full_lo = range_sm[0], full_hi = min(range_sm[1], k_end);
-  const long long pos_off = own ? p.own_pos0 : 0;
-  const View& vk = own ? p.own_k : p.k;
-  const View& vv = own ? p.own_v : p.v;
-  const uint8_t* kc = vk.codes + kvh * vk.head_codes + pos_off * (HD / 2) + t * (HD / 8);
-  const uint8_t* kx = vk.scales + kvh * vk.head_scales + pos_off * (HD / BLOCK) + t * (HD / 64);
-  const uint8_t* vc = vv.codes + kvh * vv.head_codes + pos_off * (HD / 2) + g * (HD / 16);
-  const uint8_t* vx = vv.scales + kvh * vv.head_scales + pos_off * (HD / BLOCK) + (HD == 128 ? g : g >> 1);
-  const int kg = (g >> 1) + 4 * (g & 1);   // key of M row g; row g + 8 is key kg + 8
-
-  auto fetch = [&](Raw<HD>& w, int base) {
-    const int top = k_end - 1;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const long long key = min(base + kg + 8 * i, top);
-      if constexpr (HD == 128) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4*>(kc + key * 64));
-        w.k[i][0] = u.x; w.k[i][1] = u.y; w.k[i][2] = u.z; w.k[i][3] = u.w;
-        w.ks[i] = __ldg(reinterpret_cast<const unsigned short*>(kx + key * 8));
-      } else {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(kc + key * 32));
-        w.k[i][0] = u.x; w.k[i][1] = u.y;
-        w.ks[i] = __ldg(kx + key * 4);
-      }
-    }
-    w.vs = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const long long key = min(base + t + 4 * i, top);
-      if constexpr (HD == 128) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(vc + key * 64));
-        w.v[i][0] = u.x; w.v[i][1] = u.y;
-        w.vs |= (uint32_t)__ldg(vx + key * 8) << (8 * i);
-      } else {
-        w.v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(vc + key * 32));
-        w.vs |= (uint32_t)__ldg(vx + key * 4) << (8 * i);
-      }
-    }
-  };
-
   float o[NT][KS][4], m[NT][2], l[NT][2], mult[NT][2];
   uint32_t poison = 0;
 #pragma unroll
@@ -499,12 +532,15 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
       for (int c = 0; c < 4; ++c) o[n][j][c] = 0.f;
   }
 
-  int base = k_lo + warp * STEP;
-  Raw<HD> cur, nxt;
-  if (base < k_end) fetch(cur, base);
+#pragma unroll 1
   for (; base < k_end; base += WARPS * STEP) {
-    const bool more = base + WARPS * STEP < k_end;
-    if (more) fetch(nxt, base + WARPS * STEP);
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+    __syncwarp();                          // the step has arrived for all lanes, and all are done with the one before it
+    if (base + (STAGES - 1) * WARPS * STEP < k_end) fetch((stage + STAGES - 1) % STAGES, base + (STAGES - 1) * WARPS * STEP);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    Raw<HD> cur;
+    take(cur, stage);
+    stage = (stage + 1) % STAGES;
     // ---- scores
     float s[NT][4];
 #pragma unroll
@@ -607,7 +643,6 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
         }
       }
     }
-    if (more) cur = nxt;
   }
 
   // ---- the warps' results together, in warp order
@@ -620,7 +655,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
       if (g == 0) ml_sm[warp][n * 8 + 2 * t + c] = make_float2(m[n][c], l[n][c]);
     }
   if (poison) atomicOr(&poison_sm[g], poison);
-  __syncthreads();
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();                         // the ring's place takes the results
   const bool single = parts == 1;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -683,12 +719,12 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
   if (!last_sm) return;
   __threadfence();
   float* w_sm = &o_sm[0][0][0];          // [8][MAX_PARTS] weights, then [8] 1 / sum
-  static_assert(WARPS * 8 * (HD + 4) >= 8 * MAX_PARTS + 8, "weights fit");
+  static_assert(WARPS * 8 * (HD + 4) >= 8 * MAX_PARTS + 8 + WARPS * 32 * 4, "weights and sums fit");
   for (int n = 0; n < NT; ++n) {
     __syncthreads();
     {
       const int pp = pair0 + n * 8 + warp;   // a warp per pair
-      if (pp < n_pairs) {
+      if (warp < 8 && pp < n_pairs) {
         const float2* ml = p.part_ml + ((long long)(pp / G) * p.nq + kvh * G + pp % G) * parts;
         float mx = NEG, den = 0.f;
         for (int i = lane; i < parts; i += 32) mx = fmaxf(mx, __ldcg(&ml[i]).x);
@@ -706,16 +742,28 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 2 : 1) attn_rows_kernel(
       }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 8 * (HD / 4); i += WARPS * 32) {
-      const int col = i / (HD / 4), d = i % (HD / 4) * 4, pp = pair0 + n * 8 + col;
-      if (pp >= n_pairs) continue;
+    // groups of threads share the runs between them
+    constexpr int UNITS = 8 * (HD / 4), GROUPS = WARPS * 32 / UNITS;
+    float4* red = reinterpret_cast<float4*>(w_sm + 8 * MAX_PARTS + 8);
+    const int group = threadIdx.x / UNITS, i = threadIdx.x % UNITS, col = i / (HD / 4), d = i % (HD / 4) * 4, pp = pair0 + n * 8 + col;
+    const int per = (parts + GROUPS - 1) / GROUPS;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (pp < n_pairs) {
       const float* src = p.part + ((long long)(pp / G) * p.nq + kvh * G + pp % G) * parts * HD + d;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int r = 0; r < parts; ++r) {
+#pragma unroll 10
+      for (int r = group * per; r < min(parts, (group + 1) * per); ++r) {
         const float4 v = __ldcg(reinterpret_cast<const float4*>(src + (long long)r * HD));
         const float w = w_sm[col * MAX_PARTS + r];
         a.x = fmaf(w, v.x, a.x); a.y = fmaf(w, v.y, a.y); a.z = fmaf(w, v.z, a.z); a.w = fmaf(w, v.w, a.w);
+      }
+    }
+    red[threadIdx.x] = a;
+    __syncthreads();
+    if (group == 0 && pp < n_pairs) {
+#pragma unroll
+      for (int e = 1; e < GROUPS; ++e) {
+        const float4 v = red[e * UNITS + i];
+        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
       }
       const float inv = w_sm[8 * MAX_PARTS + col];
       const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
