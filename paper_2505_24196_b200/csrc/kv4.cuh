@@ -309,9 +309,10 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 struct Scale2 {
   __half2 s, s16, m72;   // s, s / 16, -72 s
 };
-__device__ __forceinline__ Scale2 scale2(uint32_t b_lo, uint32_t b_hi) {
+// b: the scale bytes of the low and the high half at bits 0 and 16
+__device__ __forceinline__ Scale2 scale2(uint32_t b) {
   Scale2 r;
-  r.s = as_half2((b_lo << 7) | (b_hi << 23));
+  r.s = as_half2(b * 128u);
   r.s16 = __hmul2(r.s, as_half2(0x2C002C00u));    // 1 / 16
   r.m72 = __hmul2(r.s, as_half2(0xD480D480u));    // -72
   return r;
@@ -342,7 +343,7 @@ constexpr float P_BITS = 12.f;           // weights are held as 2^12 .. 2^20 x e
 
 template <int HD> struct Raw {           // one warp step: two key rows' and four value rows' pieces per lane
   uint32_t k[2][HD / 32], v[4][HD / 64];
-  uint32_t ks[2], vs;
+  uint32_t ks[2], vs[4];
 };
 template <int HD> constexpr int STEP_BYTES = STEP * (HD + HD / 8);
 template <int HD, int NT, bool SPLIT> constexpr int rows_smem() {
@@ -426,21 +427,48 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   // follow one another); of V, the 16-byte pieces of keys 2, 3 of each four are swapped in pairs (hd 128).
   constexpr int ROW = HD / 2, KV_STEP = STEP * ROW, SC = HD / BLOCK;
   const uint32_t my_ring = tc::smem_u32(ring) + warp * STAGES * STEP_BYTES<HD>;
-  auto fetch = [&](int stage, int base) {
-    const uint32_t dst = my_ring + stage * STEP_BYTES<HD>;
-#pragma unroll
-    for (int i = 0; i < ROW / 32; ++i) {
-      const int c = lane + 32 * i, key = c / (ROW / 16), piece = c % (ROW / 16);
-      const bool in = base + key < k_end;
-      const long long off = (long long)(in ? base + key : k_lo) * ROW + piece * 16;
-      const int slot = (key & 8) + ((key & 3) << 1) + ((key >> 2) & 1);
-      cp_async<16>(dst + slot * ROW + piece * 16, kc + off, in);
-      cp_async<16>(dst + KV_STEP + key * ROW + (HD == 128 ? piece ^ (key & 2) : piece) * 16, vc + off, in);
+  int ahead = k_lo + warp * STEP, ahead_stage = 0;   // the next step to fetch
+  const int f_key = HD == 128 ? lane >> 2 : lane >> 1, f_piece = HD == 128 ? lane & 3 : lane & 1, x_key = lane & 15;
+  const uint8_t* f_k = kc + (long long)(ahead + f_key) * ROW + f_piece * 16;
+  const uint8_t* f_v = vc + (long long)(ahead + f_key) * ROW + f_piece * 16;
+  const uint8_t* f_x = (lane < 16 ? kx : vx) + (long long)(ahead + x_key) * SC;
+  const uint32_t d_k = my_ring + ((f_key & 8) + ((f_key & 3) << 1) + ((f_key >> 2) & 1)) * ROW + f_piece * 16;
+  const uint32_t d_v = my_ring + KV_STEP + f_key * ROW + (HD == 128 ? f_piece ^ (f_key & 2) : f_piece) * 16;
+  const uint32_t d_x = my_ring + 2 * KV_STEP + (lane >> 4) * STEP * SC + x_key * SC;
+  auto fetch = [&]() {
+    if (ahead < k_end) {
+      const uint32_t at = ahead_stage * STEP_BYTES<HD>;
+      const bool whole = ahead + STEP <= k_end;
+      // keys past the end: zero bytes (and an address inside the cache)
+      auto copy = [&](uint32_t dst, const uint8_t* src, const uint8_t* safe, int key) {
+        const bool in = ahead + key < k_end;
+        cp_async<16>(dst + at, in ? src : safe, in);
+      };
+      if (whole) {
+        cp_async<16>(d_k + at, f_k, true);
+        cp_async<16>(d_v + at, f_v, true);
+        if constexpr (HD == 128) {     // eight keys further on
+          cp_async<16>(d_k + at + 8 * ROW, f_k + 8 * ROW, true);
+          cp_async<16>(d_v + at + 8 * ROW, f_v + 8 * ROW, true);
+        }
+        cp_async<SC>(d_x + at, f_x, true);
+      } else {
+        copy(d_k, f_k, kc + (long long)k_lo * ROW, f_key);
+        copy(d_v, f_v, vc + (long long)k_lo * ROW, f_key);
+        if constexpr (HD == 128) {
+          copy(d_k + 8 * ROW, f_k + 8 * ROW, kc + (long long)k_lo * ROW, f_key + 8);
+          copy(d_v + 8 * ROW, f_v + 8 * ROW, vc + (long long)k_lo * ROW, f_key + 8);
+        }
+        const bool in = ahead + x_key < k_end;
+        cp_async<SC>(d_x + at, in ? f_x : (lane < 16 ? kx : vx) + (long long)k_lo * SC, in);
+      }
+      ahead += WARPS * STEP;
+      f_k += WARPS * STEP * ROW;
+      f_v += WARPS * STEP * ROW;
+      f_x += WARPS * STEP * SC;
+      if (++ahead_stage == STAGES) ahead_stage = 0;
     }
-    const int key = lane & 15;
-    const bool in = base + key < k_end;
-    cp_async<SC>(dst + 2 * KV_STEP + (lane >> 4) * STEP * SC + key * SC,
-                 (lane < 16 ? kx : vx) + (long long)(in ? base + key : k_lo) * SC, in);
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
   auto take = [&](Raw<HD>& w, int stage) {
     const uint8_t* s = ring + (warp * STAGES + stage) * STEP_BYTES<HD>;
@@ -458,7 +486,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
         w.ks[i] = *x;
       }
     }
-    w.vs = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int key = t + 4 * i;
@@ -469,16 +496,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
       } else {
         w.v[i][0] = *reinterpret_cast<const uint32_t*>(a + g * 4);
       }
-      w.vs |= (uint32_t)s[2 * KV_STEP + STEP * SC + key * SC + (HD == 128 ? g : g >> 1)] << (8 * i);
+      w.vs[i] = s[2 * KV_STEP + STEP * SC + key * SC + (HD == 128 ? g : g >> 1)];
     }
   };
 
   int base = k_lo + warp * STEP, stage = 0;
-#pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i) {
-    if (base + i * WARPS * STEP < k_end) fetch(i, base + i * WARPS * STEP);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  }
+#pragma unroll 1
+  for (int i = 0; i < STAGES - 1; ++i) fetch();
 
   // q rows into the fragments of the second operand: a warp per pair, lane = its place along the row
   for (int i = warp; i < PB; i += WARPS) {
@@ -536,22 +560,22 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   for (; base < k_end; base += WARPS * STEP) {
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
     __syncwarp();                          // the step has arrived for all lanes, and all are done with the one before it
-    if (base + (STAGES - 1) * WARPS * STEP < k_end) fetch((stage + STAGES - 1) % STAGES, base + (STAGES - 1) * WARPS * STEP);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    fetch();
     Raw<HD> cur;
     take(cur, stage);
-    stage = (stage + 1) % STAGES;
+    if (++stage == STAGES) stage = 0;
     // ---- scores
-    float s[NT][4];
+    // (two chains of multiplies, whatever NT: a row is the same bits)
+    float s[NT][4], s2[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[n][c] = 0.f;
+      for (int c = 0; c < 4; ++c) s[n][c] = s2[n][c] = 0.f;
 #pragma unroll
     for (int wd = 0; wd < KW; ++wd) {
-      const int sh = HD == 128 ? (wd >> 1) * 8 : 0;   // two words per scale
-      const uint32_t b0 = (cur.ks[0] >> sh) & 255u, b1 = (cur.ks[1] >> sh) & 255u;
-      const Scale2 s0 = scale2(b0, b0), s1 = scale2(b1, b1);
+      constexpr int WPS = 2;                          // words per scale
+      const Scale2 s0 = scale2(__byte_perm(cur.ks[0], 0, 0x4040 + 0x101 * (wd / WPS))),
+                   s1 = scale2(__byte_perm(cur.ks[1], 0, 0x4040 + 0x101 * (wd / WPS)));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t w0 = cur.k[0][wd] >> (8 * h), w1 = cur.k[1][wd] >> (8 * h);
@@ -561,7 +585,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
 #pragma unroll
           for (int q = 0; q < PARTS; ++q) {
             const uint2 b = qf[q][n][wd * 2 + h][lane];
-            mma16816(s[n], a, b.x, b.y);
+            mma16816(h ? s2[n] : s[n], a, b.x, b.y);
           }
       }
     }
@@ -571,7 +595,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[n][c] *= mult[n][c & 1];
+      for (int c = 0; c < 4; ++c) s[n][c] = (s[n][c] + s2[n][c]) * mult[n][c & 1];
       if (!full) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -614,18 +638,21 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
       }
     }
     // ---- values.  Lane (g, t): keys t, t + 4 are the M-operand's columns 2 t, 2 t + 1, keys t + 8, t + 12 the upper ones
-    if (__vcmpeq4(cur.vs, 0xffffffffu)) {
-#pragma unroll 1
+    Scale2 z0 = scale2(cur.vs[0] + cur.vs[1] * 65536u), z1 = scale2(cur.vs[2] + cur.vs[3] * 65536u);
+    const __half2 zz = __hadd2(z0.s, z1.s);             // NaN where one of the four is
+    if (!__hbeq2(zz, zz)) {
+#pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (((cur.vs >> (8 * i)) & 255u) == NAN_SCALE) {
+        if (cur.vs[i] == NAN_SCALE) {
           const int key = base + t + 4 * i;
 #pragma unroll 1
           for (int c = 0; c < PB; ++c)
             if (key >= lo_sm[c] && key < min(hi_sm[c], k_end)) poison |= 1u << c;
-          cur.vs &= ~(255u << (8 * i));
+          cur.vs[i] = 0;
         }
+      z0 = scale2(cur.vs[0] + cur.vs[1] * 65536u);
+      z1 = scale2(cur.vs[2] + cur.vs[3] * 65536u);
     }
-    const Scale2 z0 = scale2(cur.vs & 255u, (cur.vs >> 8) & 255u), z1 = scale2((cur.vs >> 16) & 255u, cur.vs >> 24);
 #pragma unroll
     for (int wd = 0; wd < VW; ++wd) {
 #pragma unroll
@@ -922,8 +949,7 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
       if (value) {
 #pragma unroll
         for (int k = 0; k < W; ++k) {
-          const uint32_t sb = (d.s >> (8 * (k >> 1))) & 255u;
-          const Scale2 sc = scale2(sb, sb);
+          const Scale2 sc = scale2(__byte_perm(d.s, 0, 0x4040 + 0x101 * (k >> 1)));
           const uint32_t w = d.w[k], w8 = w >> 8;
           put(k, nib_lo(w, sc), nib_hi(w, sc), nib_lo(w8, sc), nib_hi(w8, sc));
         }
