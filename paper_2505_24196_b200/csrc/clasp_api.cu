@@ -41,6 +41,7 @@ constexpr long long S32_MAX_SCORES = 65536;   // rows x query heads x keys
 constexpr int WIDE_MIN_ROWS = 128;   // layers over more rows take the products and the attention of wide.cuh
 constexpr int KV4_MAX_CTX = 1 << 30;   // positions of a 4-bit cache: key numbers and steps past the end stay in 32 bits
 constexpr int KV4_ROWS = 64;           // rows per launch of the attention of few rows: bounds its workspace
+constexpr int KV4_MIN_STEPS = 4;       // steps a warp takes in a full run at least: joining two runs costs about as much
 constexpr int KV4_FEW_ROWS = 16;       // rows of a call (bf16) whose sums do not depend on how many share it
 constexpr size_t KV4_MANY_SLOTS = 160 * 256;   // (pair, part) slots of the attention of many rows: about one CTA's pairs per SM
 constexpr int MAX_COUNTERS = 4096;   // tiles of one GEMM launch that may use split-K
@@ -125,7 +126,7 @@ bool is_kv4(const clasp_config& c) { return (c.flags & CLASP_FLAG_KV4) != 0; }
 int kv4_run_len(const clasp_config& c) {
   const int step = clasp::kv4::WARPS * clasp::kv4::STEP;
   const int target = std::max(1, std::min(clasp::kv4::MAX_PARTS - 4, 148 / c.n_kv_heads));
-  return std::max(1, ((c.max_ctx + target - 1) / target + step - 1) / step) * step;
+  return std::max(KV4_MIN_STEPS, ((c.max_ctx + target - 1) / target + step - 1) / step) * step;
 }
 int kv4_max_parts(const clasp_config& c) {
   const int len = kv4_run_len(c);

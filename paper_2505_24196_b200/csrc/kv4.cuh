@@ -230,8 +230,7 @@ __device__ __forceinline__ int row_limit(const AttnArgs& p, int r) {
 }
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -259,7 +258,7 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t o) {
   return y;
 }
 
-// A query row for half precision: the power of two that brings its largest magnitude into [2^13, 2^14), and
+// A query row for half precision: the power of two that brings its largest magnitude into [2^9, 2^10), and
 // the factor that takes it back and brings the scores into units of log2 (1 / sqrt(hd) aside).  LANES neighbouring lanes hold a row,
 // N values each.  A row with an infinity or NaN in it has no finite score: its factor is NaN, and so are all its weights.
 struct RowScale {
@@ -267,7 +266,7 @@ struct RowScale {
 };
 // a: the bits of the row's largest magnitude
 __device__ __forceinline__ RowScale scale_for(uint32_t a) {
-  const int up = 13 - max((int)(a >> 23) - 127, -113);   // rows far below 2^-113 are as good as zero
+  const int up = 9 - max((int)(a >> 23) - 127, -113);   // rows far below 2^-113 are as good as zero
   RowScale r;
 
   r.up = __uint_as_float((uint32_t)(127 + up) << 23);
@@ -307,21 +306,25 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 
 // Scales of the two halves of a register, as the conversion needs them.
 struct Scale2 {
-  __half2 s, s16, m72;   // s, s / 16, -72 s
+  __half2 s, s16, m64, m72;   // s, s / 16, -64.5 s, -72 s
 };
 // b: the scale bytes of the low and the high half at bits 0 and 16
 __device__ __forceinline__ Scale2 scale2(uint32_t b) {
   Scale2 r;
   r.s = as_half2(b * 128u);
   r.s16 = __hmul2(r.s, as_half2(0x2C002C00u));    // 1 / 16
+  r.m64 = __hmul2(r.s, as_half2(0xD408D408u));    // -64.5
   r.m72 = __hmul2(r.s, as_half2(0xD480D480u));    // -72
   return r;
 }
-// The nibbles 0, 1 (w) or 2, 3 (w >> 8) of both 16-bit halves as values (c - 8) s.  A nibble in the low mantissa bits of
-// 1024 makes 1024 + c, one place higher 1024 + 16 c: no integer conversion.  Exact: c - 8 and its product with s have
-// few bits; 72 s has 7 (9 x a 4-bit mantissa).  (1024 + c) s - 1032 s in one step would overflow from s = 64 on.
+// The nibbles 0, 1 (w) or 2, 3 (w >> 8) of both 16-bit halves: a nibble in the low mantissa bits of 1024 makes 1024 + c, one
+// place higher 1024 + 16 c, without an integer conversion; one multiply-add with s / 16 then gives
+//   nib_lo: (c - 8) s / 16     nib_hi: (c - 8) s
+// exactly (64.5 s and 72 s have at most 11 significant bits, the results at most 7 above half precision's last place).  The
+// sixteenth is made up for where it costs nothing: in q, and in the finished output.  ((1024 + c) s - 1032 s would overflow
+// from s = 64 on.)
 __device__ __forceinline__ uint32_t nib_lo(uint32_t w, const Scale2& s) {
-  return as_u32(__hmul2(__hsub2(as_half2(and_or(w, 0x000F000Fu, 0x64006400u)), as_half2(0x64086408u)), s.s));
+  return as_u32(__hfma2(as_half2(and_or(w, 0x000F000Fu, 0x64006400u)), s.s16, s.m64));
 }
 __device__ __forceinline__ uint32_t nib_hi(uint32_t w, const Scale2& s) {
   return as_u32(__hfma2(as_half2(and_or(w, 0x00F000F0u, 0x64006400u)), s.s16, s.m72));
@@ -365,8 +368,8 @@ template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const vo
 // K and V in 16- and 8-byte loads and converts them in place: lane (g, t) of a step holds dims [32 t, 32 t + 32) of two keys, and
 // 16 dims [16 g, 16 g + 16) of four values (hd 128).  A warp copies its steps to a ring of its own, three ahead (asynchronous
 // copies: the bytes on their way cost no registers), with the rows placed so that those loads meet no bank twice.  K and V are exact in
-// half precision.  q is scaled by a power of two per row to a largest magnitude in [2^13, 2^14) and rounded to half precision:
-// exact for bf16 rows (what lies 2^24 below the row's maximum aside); SPLIT (fp32 models) adds the rounding error of q and of
+// half precision.  q is scaled by a power of two per row to a largest magnitude in [2^9, 2^10) (a nibble's 16 on top of it, see nib_lo) and
+// rounded to half precision: exact for bf16 rows (what lies 2^25 below the row's maximum aside); SPLIT (fp32 models) adds the rounding error of q and of
 // the weights as a second half-precision operand: 22 bits.  Weights: half precision of 2^12 exp2(s - m), m a maximum that moves
 // only when exceeded by 2^3, so they stay below 2^15 and lose nothing above 2^-26 of the largest; sums in fp32.
 // A block with the NaN byte must reach only the rows that see it, and 0 x NaN is NaN: values' NaN blocks enter as zeros, and
@@ -532,6 +535,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
     for (int e = 0; e < E; ++e) {
       const int d = lane * E + e, tt = d / (HD / 4), wd = d % (HD / 4) / 8, n = d & 7;
       const int step = wd * 2 + ((n >> 1) & 1);
+      if ((n & 1) == 0) x[e] *= 16.f;    // meets nib_lo
       const __half hx = __float2half_rn(x[e]);
       __half* dst = reinterpret_cast<__half*>(&qf[0][i >> 3][step][(i & 7) * 4 + tt]) + (n & 1) * 2 + (n >> 2);
       *dst = hx;
@@ -544,12 +548,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   }
   __syncthreads();
 
-  float o[NT][KS][4], m[NT][2], l[NT][2], mult[NT][2];
+  // off: m - P_BITS of each pair (0 before its first visible key, then top is -inf); top: a score above it moves m
+  float o[NT][KS][4], off[NT][2], top[NT][2], l[NT][2], mult[NT][2];
   uint32_t poison = 0;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) { m[n][c] = NEG; l[n][c] = 0.f; mult[n][c] = mult_sm[n * 8 + 2 * t + c]; }
+    for (int c = 0; c < 2; ++c) { off[n][c] = 0.f; top[n][c] = NEG; l[n][c] = 0.f; mult[n][c] = mult_sm[n * 8 + 2 * t + c]; }
 #pragma unroll
     for (int j = 0; j < KS; ++j)
 #pragma unroll
@@ -595,7 +600,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[n][c] = (s[n][c] + s2[n][c]) * mult[n][c & 1];
+      for (int c = 0; c < 4; ++c) s[n][c] = fmaf(s2[n][c], mult[n][c & 1], fmaf(s[n][c], mult[n][c & 1], -off[n][c & 1]));
       if (!full) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -604,16 +609,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
         }
       }
       const float x0 = fmaxf(s[n][0], s[n][2]), x1 = fmaxf(s[n][1], s[n][3]);
-      if (__any_sync(0xffffffffu, x0 > m[n][0] + 3.f || x1 > m[n][1] + 3.f)) {
+      if (__any_sync(0xffffffffu, x0 > top[n][0] || x1 > top[n][1])) {
         float y[2] = {x0, x1};
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) y[c] = fmaxf(y[c], __shfl_xor_sync(0xffffffffu, y[c], d));
-          if (y[c] > m[n][c] + 3.f) {
-            const float corr = exp2f(m[n][c] - y[c]);
-            m[n][c] = y[c];
+          if (y[c] > top[n][c]) {
+            const float by = y[c] - P_BITS, corr = top[n][c] == NEG ? 0.f : exp2f(-by);
+            off[n][c] += by;
+            top[n][c] = P_BITS + 3.f;
             l[n][c] *= corr;
+            s[n][c] -= by;
+            s[n][c + 2] -= by;
 #pragma unroll
             for (int j = 0; j < KS; ++j) { o[n][j][c] *= corr; o[n][j][c + 2] *= corr; }
           }
@@ -621,10 +629,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
       }
       float e[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float mm = m[n][c & 1] == NEG ? 0.f : m[n][c & 1] - P_BITS;   // no visible key so far: exp2(-inf) = 0
-        e[c] = ex2(s[n][c] - mm);
-      }
+      for (int c = 0; c < 4; ++c) e[c] = ex2(s[n][c]);   // (nothing visible so far: exp2(-inf) = 0)
       l[n][0] += e[0] + e[2];
       l[n][1] += e[1] + e[3];
 #pragma unroll
@@ -673,10 +678,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   }
 
   // ---- the warps' results together, in warp order
+  float m[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
+      m[n][c] = top[n][c] == NEG ? NEG : off[n][c];   // (in every part alike without P_BITS)
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
       if (g == 0) ml_sm[warp][n * 8 + 2 * t + c] = make_float2(m[n][c], l[n][c]);
@@ -698,7 +705,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
       const bool bad = (poison_sm[g] >> (n * 8 + col)) & 1u;
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        float2 v = make_float2(o[n][j][c] * corr, o[n][j][c + 2] * corr);
+        float2 v = make_float2(o[n][j][c] * (corr * 16.f), o[n][j][c + 2] * corr);   // (even dims are nib_lo's)
         if (m[n][c] == NEG && l[n][c] == 0.f) v = make_float2(0.f, 0.f);
         if (bad) v = make_float2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
         *reinterpret_cast<float2*>(&o_sm[warp][col][g * (HD / 8) + 2 * j]) = v;
@@ -1215,8 +1222,8 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
         float f[32];
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-          const int dim = (k & ~7) + ((k & 1) << 2) + ((k & 7) >> 1);   // columns hold dims 0 4 1 5 2 6 3 7 of each eight
-          f[dim] = ((bad >> ((c + k) >> 4)) & 1u) ? __int_as_float(0x7fffffff) : o[k] * inv;
+          const int dim = (k & ~7) + ((k & 1) << 2) + ((k & 7) >> 1);   // columns hold dims 0 4 1 5 2 6 3 7 of each eight, 0 4 2 6 as sixteenths
+          f[dim] = ((bad >> ((c + k) >> 4)) & 1u) ? __int_as_float(0x7fffffff) : o[k] * ((k & 2) ? inv : inv * 16.f);
         }
         if (part) {
 #pragma unroll
