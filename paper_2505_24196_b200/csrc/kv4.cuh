@@ -350,7 +350,7 @@ template <int HD> struct Raw {           // one warp step: two key rows' and fou
 };
 template <int HD> constexpr int STEP_BYTES = STEP * (HD + HD / 8);
 template <int HD, int NT, bool SPLIT> constexpr int rows_smem() {
-  constexpr int ring = WARPS * STAGES * STEP_BYTES<HD>, merge = WARPS * 8 * (HD + 4) * 4;
+  constexpr int ring = WARPS * STAGES * STEP_BYTES<HD>, merge = WARPS * 8 * NT * (HD + 4) * 4;
   return (ring > merge ? ring : merge) + (SPLIT ? 2 : 1) * NT * (HD / 16) * 32 * 8;
 }
 template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool in) {
@@ -384,8 +384,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   extern __shared__ __align__(1024) uint8_t smem[];
   uint2 (*qf)[NT][KS][32] = reinterpret_cast<uint2 (*)[NT][KS][32]>(smem);
   uint8_t* ring = smem + PARTS * NT * KS * 32 * 8;                       // the warps' steps, later their results
-  float (*o_sm)[8][HD + 4] = reinterpret_cast<float (*)[8][HD + 4]>(ring);
+  float (*o_sm)[PB][HD + 4] = reinterpret_cast<float (*)[PB][HD + 4]>(ring);
   __shared__ float2 ml_sm[WARPS][PB];
+  __shared__ float w_sm[WARPS][PB], mx_sm[PB];
   __shared__ float mult_sm[PB];
   __shared__ int lo_sm[PB], hi_sm[PB];
   __shared__ uint32_t poison_sm[8];
@@ -677,65 +678,63 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
     }
   }
 
-  // ---- the warps' results together, in warp order
-  float m[NT][2];
+  // ---- the warps' results together, in warp order.  (From here on every instruction runs once: short code, its fetch counts.)
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();                         // the ring's place takes the results
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      m[n][c] = top[n][c] == NEG ? NEG : off[n][c];   // (in every part alike without P_BITS)
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
-      if (g == 0) ml_sm[warp][n * 8 + 2 * t + c] = make_float2(m[n][c], l[n][c]);
+      // (maxima without P_BITS, here and in every part alike; a sum without a maximum is 0, or NaN)
+      if (g == 0) ml_sm[warp][n * 8 + 2 * t + c] = make_float2(top[n][c] == NEG ? NEG : off[n][c], l[n][c]);
+#pragma unroll
+      for (int j = 0; j < KS; ++j)
+        *reinterpret_cast<float2*>(&o_sm[warp][n * 8 + 2 * t + c][g * (HD / 8) + 2 * j]) =
+            make_float2(o[n][j][c] * 16.f, o[n][j][c + 2]);   // (even dims are nib_lo's)
     }
   if (poison) atomicOr(&poison_sm[g], poison);
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();                         // the ring's place takes the results
+  __syncthreads();
+  constexpr int UNITS = PB * (HD / 4), GROUPS = WARPS * 32 / UNITS;   // four dims of a pair; threads that share the work on them
+  static_assert(WARPS * PB <= WARPS * 32 && GROUPS >= 1, "a thread per (warp, pair), one at least per unit");
+  if (threadIdx.x < WARPS * PB) {          // each warp's weight
+    const int col = threadIdx.x % PB, w = threadIdx.x / PB;
+    float mx = NEG;
+#pragma unroll 4
+    for (int i = 0; i < WARPS; ++i) mx = fmaxf(mx, ml_sm[i][col].x);
+    const float2 v = ml_sm[w][col];
+    w_sm[w][col] = v.x == NEG ? (v.y == 0.f ? 0.f : 1.f) : exp2f(v.x - mx);
+    if (w == 0) mx_sm[col] = mx;
+  }
+  __syncthreads();
   const bool single = parts == 1;
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    if (n > 0) __syncthreads();
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int col = 2 * t + c;
-      float mx = NEG;
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, ml_sm[w][n * 8 + col].x);
-      const float corr = m[n][c] == NEG ? 0.f : exp2f(m[n][c] - mx);
-      const bool bad = (poison_sm[g] >> (n * 8 + col)) & 1u;
-#pragma unroll
-      for (int j = 0; j < KS; ++j) {
-        float2 v = make_float2(o[n][j][c] * (corr * 16.f), o[n][j][c + 2] * corr);   // (even dims are nib_lo's)
-        if (m[n][c] == NEG && l[n][c] == 0.f) v = make_float2(0.f, 0.f);
-        if (bad) v = make_float2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
-        *reinterpret_cast<float2*>(&o_sm[warp][col][g * (HD / 8) + 2 * j]) = v;
-      }
+  const int unit = threadIdx.x % UNITS, group = threadIdx.x / UNITS, col = unit / (HD / 4), d = unit % (HD / 4) * 4;
+  const int pp = pair0 + col, r = pp / G, hq = kvh * G + pp - r * G;
+  const bool on = pp < n_pairs;
+  const long long rh = (long long)r * p.nq + hq;
+  auto store = [&](const float4& a, float den) {
+    const float inv = den == 0.f ? 0.f : 1.0f / den;
+    const long long at = (long long)r * p.out_stride + (long long)hq * HD + d;
+    if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + at) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+    else *reinterpret_cast<float4*>((float*)p.out + at) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+  };
+  if (group == 0 && on) {
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float den = 0.f;
+#pragma unroll 4
+    for (int w = 0; w < WARPS; ++w) {
+      const float4 v = *reinterpret_cast<const float4*>(&o_sm[w][col][d]);
+      const float f = w_sm[w][col];
+      a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
+      den = fmaf(f, ml_sm[w][col].y, den);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 8 * (HD / 4); i += WARPS * 32) {
-      const int col = i / (HD / 4), d = i % (HD / 4) * 4, pp = pair0 + n * 8 + col;
-      if (pp >= n_pairs) continue;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      float mx = NEG, den = 0.f;
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, ml_sm[w][n * 8 + col].x);
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float4 v = *reinterpret_cast<const float4*>(&o_sm[w][col][d]);
-        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
-        const float2 ml = ml_sm[w][n * 8 + col];
-        den += ml.x == NEG ? ml.y : ml.y * exp2f(ml.x - mx);   // (a sum without a maximum is 0, or NaN)
-      }
-      const long long rh = (long long)(pp / G) * p.nq + kvh * G + pp % G;
-      if (single) {
-        const float inv = den == 0.f ? 0.f : 1.0f / den;
-        const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
-        if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
-        else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
-      } else {
-        *reinterpret_cast<float4*>(p.part + (rh * parts + run) * HD + d) = a;
-        if (d == 0) p.part_ml[rh * parts + run] = make_float2(mx, den);
-      }
+    if ((poison_sm[d / (HD / 8)] >> col) & 1u) a.x = a.y = a.z = a.w = __int_as_float(0x7fffffff);
+    if (single) {
+      store(a, den);
+    } else {
+      *reinterpret_cast<float4*>(p.part + (rh * parts + run) * HD + d) = a;
+      if (d == 0) p.part_ml[rh * parts + run] = make_float2(mx_sm[col], den);
     }
   }
   if (single) return;
@@ -752,59 +751,53 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   __syncthreads();
   if (!last_sm) return;
   __threadfence();
-  float* w_sm = &o_sm[0][0][0];          // [8][MAX_PARTS] weights, then [8] 1 / sum
-  static_assert(WARPS * 8 * (HD + 4) >= 8 * MAX_PARTS + 8 + WARPS * 32 * 4, "weights and sums fit");
-  for (int n = 0; n < NT; ++n) {
-    __syncthreads();
-    {
-      const int pp = pair0 + n * 8 + warp;   // a warp per pair
-      if (warp < 8 && pp < n_pairs) {
-        const float2* ml = p.part_ml + ((long long)(pp / G) * p.nq + kvh * G + pp % G) * parts;
-        float mx = NEG, den = 0.f;
-        for (int i = lane; i < parts; i += 32) mx = fmaxf(mx, __ldcg(&ml[i]).x);
+  float* wr_sm = reinterpret_cast<float*>(ring);                       // [PB][MAX_PARTS] weights of the runs
+  float* den_sm = wr_sm + PB * MAX_PARTS;                              // [PB]
+  float4* red = reinterpret_cast<float4*>(den_sm + PB);                // [threads]
+  static_assert(WARPS * PB * (HD + 4) >= PB * MAX_PARTS + PB + WARPS * 32 * 4, "weights and sums fit");
+  if (warp < PB && pair0 + warp < n_pairs) {                           // a warp per pair
+    const int rw = (pair0 + warp) / G;
+    const float2* ml = p.part_ml + ((long long)rw * p.nq + kvh * G + pair0 + warp - rw * G) * parts;
+    float mx = NEG, den = 0.f;
+#pragma unroll 1
+    for (int i = lane; i < parts; i += 32) mx = fmaxf(mx, __ldcg(&ml[i]).x);
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        for (int i = lane; i < parts; i += 32) {
-          const float2 v = __ldcg(&ml[i]);
-          const float w = v.x == NEG ? (v.y == 0.f ? 0.f : 1.f) : exp2f(v.x - mx);
-          w_sm[warp * MAX_PARTS + i] = w;
-          den += v.y * w;
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) den += __shfl_xor_sync(0xffffffffu, den, d);
-        if (lane == 0) w_sm[8 * MAX_PARTS + warp] = den == 0.f ? 0.f : 1.0f / den;
-      }
+    for (int e = 16; e > 0; e >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, e));
+#pragma unroll 1
+    for (int i = lane; i < parts; i += 32) {
+      const float2 v = __ldcg(&ml[i]);
+      const float w = v.x == NEG ? (v.y == 0.f ? 0.f : 1.f) : exp2f(v.x - mx);
+      wr_sm[warp * MAX_PARTS + i] = w;
+      den = fmaf(v.y, w, den);
     }
-    __syncthreads();
-    // groups of threads share the runs between them
-    constexpr int UNITS = 8 * (HD / 4), GROUPS = WARPS * 32 / UNITS;
-    float4* red = reinterpret_cast<float4*>(w_sm + 8 * MAX_PARTS + 8);
-    const int group = threadIdx.x / UNITS, i = threadIdx.x % UNITS, col = i / (HD / 4), d = i % (HD / 4) * 4, pp = pair0 + n * 8 + col;
-    const int per = (parts + GROUPS - 1) / GROUPS;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (pp < n_pairs) {
-      const float* src = p.part + ((long long)(pp / G) * p.nq + kvh * G + pp % G) * parts * HD + d;
-#pragma unroll 10
-      for (int r = group * per; r < min(parts, (group + 1) * per); ++r) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + (long long)r * HD));
-        const float w = w_sm[col * MAX_PARTS + r];
-        a.x = fmaf(w, v.x, a.x); a.y = fmaf(w, v.y, a.y); a.z = fmaf(w, v.z, a.z); a.w = fmaf(w, v.w, a.w);
-      }
-    }
-    red[threadIdx.x] = a;
-    __syncthreads();
-    if (group == 0 && pp < n_pairs) {
 #pragma unroll
-      for (int e = 1; e < GROUPS; ++e) {
-        const float4 v = red[e * UNITS + i];
-        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
-      }
-      const float inv = w_sm[8 * MAX_PARTS + col];
-      const long long off = (long long)(pp / G) * p.out_stride + (long long)(kvh * G + pp % G) * HD + d;
-      if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + off) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
-      else *reinterpret_cast<float4*>((float*)p.out + off) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    for (int e = 16; e > 0; e >>= 1) den += __shfl_xor_sync(0xffffffffu, den, e);
+    if (lane == 0) den_sm[warp] = den;
+  }
+  __syncthreads();
+  // groups of threads share the runs between them
+  const int per = (parts + GROUPS - 1) / GROUPS, last_run = min(parts, (group + 1) * per);
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (on) {
+    const float* src = p.part + rh * parts * HD + d;
+#pragma unroll 9
+    for (int i = group * per; i < last_run; ++i) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(src + (long long)i * HD));
+      const float w = wr_sm[col * MAX_PARTS + i];
+      a.x = fmaf(w, v.x, a.x); a.y = fmaf(w, v.y, a.y); a.z = fmaf(w, v.z, a.z); a.w = fmaf(w, v.w, a.w);
     }
   }
+  if constexpr (GROUPS > 1) {
+    red[threadIdx.x] = a;
+    __syncthreads();
+    if (group > 0 || !on) return;
+#pragma unroll
+    for (int e = 1; e < GROUPS; ++e) {
+      const float4 v = red[e * UNITS + unit];
+      a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+    }
+  }
+  if (on) store(a, den_sm[col]);
 }
 
 // ------------------------------------------------------------------ attention of many pairs
