@@ -203,6 +203,7 @@ class Clasp:
         if nbytes == 0:
             raise ClaspError(-2, "clasp_workspace_bytes")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self._dev, self._stream_ptr = self.workspace.device, self.stream.cuda_stream
         handle = C.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.lib.clasp_create(C.byref(cfg), self.workspace.data_ptr(), nbytes,
@@ -318,17 +319,18 @@ class Clasp:
     def _head_rows(self, t: torch.Tensor, heads: int, what: str) -> int:
         """Stride in elements of rows [n, heads, head_dim] in the model dtype; the heads of a row are contiguous."""
         hd = self.cfg.head_dim
-        if t.dtype != self.dtype or t.device != self.workspace.device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != hd:
-            raise ValueError(f"{what}: [n, {heads}, {hd}] {self.dtype} on {self.workspace.device} expected")
+        shape = t.shape
+        if len(shape) != 3 or shape[1] != heads or shape[2] != hd or t.dtype != self.dtype or t.device != self._dev:
+            raise ValueError(f"{what}: [n, {heads}, {hd}] {self.dtype} on {self._dev} expected")
         sr, sh, sd = t.stride()
-        if (sd != 1 or (sh != hd and heads > 1)) and t.shape[0]:
+        if (sd != 1 or (sh != hd and heads > 1)) and shape[0]:
             raise ValueError(f"{what}: the heads of a row must be contiguous")
-        return sr if t.shape[0] > 1 else max(sr, heads * hd)
+        return sr if shape[0] > 1 else max(sr, heads * hd)
 
     def _new_rows(self, *shape: int) -> torch.Tensor:
-        t = torch.empty(shape, dtype=self.dtype, device=self.workspace.device)
+        t = torch.empty(shape, dtype=self.dtype, device=self._dev)
         # memory handed out for another stream than the one that fills it
-        if torch._C._cuda_getCurrentRawStream(self.workspace.device.index) != self.stream.cuda_stream:
+        if torch._C._cuda_getCurrentRawStream(self._dev.index) != self._stream_ptr:
             t.record_stream(self.stream)
         return t
 
@@ -358,11 +360,13 @@ class Clasp:
             raise ValueError("n: a number of rows")
         if k_out is None and v_out is None:
             k_out, v_out = self._new_rows(2, n, h, self.cfg.head_dim).unbind(0)
-        k_out = self._new_rows(n, h, self.cfg.head_dim) if k_out is None else k_out
-        v_out = self._new_rows(n, h, self.cfg.head_dim) if v_out is None else v_out
-        ks, vs = self._head_rows(k_out, h, "k_out"), self._head_rows(v_out, h, "v_out")
-        if k_out.shape[0] != n or v_out.shape[0] != n:
-            raise ValueError("k_out, v_out: n rows")
+            ks = vs = h * self.cfg.head_dim
+        else:
+            k_out = self._new_rows(n, h, self.cfg.head_dim) if k_out is None else k_out
+            v_out = self._new_rows(n, h, self.cfg.head_dim) if v_out is None else v_out
+            ks, vs = self._head_rows(k_out, h, "k_out"), self._head_rows(v_out, h, "v_out")
+            if k_out.shape[0] != n or v_out.shape[0] != n:
+                raise ValueError("k_out, v_out: n rows")
         _check(self.lib.clasp_kv4_read(self.handle, self._kv4_layer(kv, layer), pos0, n, k_out.data_ptr(), ks, v_out.data_ptr(),
                                        vs), "clasp_kv4_read")
         return k_out, v_out

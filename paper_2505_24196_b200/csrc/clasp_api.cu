@@ -219,10 +219,8 @@ cudaError_t kv4_attributes() {
   const struct { const void* f; int bytes; } k[] = {
       {(const void*)k4::attn_many_kernel<128, 1>, k4::many_smem<128, 1>()}, {(const void*)k4::attn_many_kernel<128, 2>, k4::many_smem<128, 2>()},
       {(const void*)k4::attn_many_kernel<64, 1>, k4::many_smem<64, 1>()}, {(const void*)k4::attn_many_kernel<64, 2>, k4::many_smem<64, 2>()},
-      {(const void*)k4::attn_rows_kernel<128, 1, false>, k4::rows_smem<128, 1, false>()}, {(const void*)k4::attn_rows_kernel<128, 2, false>, k4::rows_smem<128, 2, false>()},
-      {(const void*)k4::attn_rows_kernel<128, 1, true>, k4::rows_smem<128, 1, true>()}, {(const void*)k4::attn_rows_kernel<128, 2, true>, k4::rows_smem<128, 2, true>()},
-      {(const void*)k4::attn_rows_kernel<64, 1, false>, k4::rows_smem<64, 1, false>()}, {(const void*)k4::attn_rows_kernel<64, 2, false>, k4::rows_smem<64, 2, false>()},
-      {(const void*)k4::attn_rows_kernel<64, 1, true>, k4::rows_smem<64, 1, true>()}, {(const void*)k4::attn_rows_kernel<64, 2, true>, k4::rows_smem<64, 2, true>()}};
+      {(const void*)k4::attn_rows_kernel<128, false>, k4::rows_smem<128, false>()}, {(const void*)k4::attn_rows_kernel<128, true>, k4::rows_smem<128, true>()},
+      {(const void*)k4::attn_rows_kernel<64, false>, k4::rows_smem<64, false>()}, {(const void*)k4::attn_rows_kernel<64, true>, k4::rows_smem<64, true>()}};
   for (const auto& e : k) {
     const cudaError_t rc = cudaFuncSetAttribute(e.f, cudaFuncAttributeMaxDynamicSharedMemorySize, e.bytes);
     if (rc != cudaSuccess) return rc;
@@ -613,12 +611,8 @@ template <int HD, bool SPLIT>
 int kv4_rows_launch(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
   namespace k4 = clasp::kv4;
   const int pairs = p.R * (p.nq / p.nkv);
-  // eight or sixteen pairs per CTA (a block of pairs reads the run again: at sixteen the multiplies weigh as much as the
-  // conversion, and 24 or 32 would need more registers than sixteen warps leave)
-  const int nt = pairs <= 8 ? 1 : 2;
-  const dim3 grid(p.runs + (p.own_n > 0 ? 1 : 0), p.nkv, (pairs + 8 * nt - 1) / (8 * nt));
-  if (nt == 1) k4::attn_rows_kernel<HD, 1, SPLIT><<<grid, k4::WARPS * 32, k4::rows_smem<HD, 1, SPLIT>(), ctx->stream>>>(p);
-  else k4::attn_rows_kernel<HD, 2, SPLIT><<<grid, k4::WARPS * 32, k4::rows_smem<HD, 2, SPLIT>(), ctx->stream>>>(p);
+  const dim3 grid(p.runs + (p.own_n > 0 ? 1 : 0), p.nkv, (pairs + 7) / 8);
+  k4::attn_rows_kernel<HD, SPLIT><<<grid, k4::WARPS * 32, k4::rows_smem<HD, SPLIT>(), ctx->stream>>>(p);
   return launch_check(ctx);
 }
 
@@ -1917,6 +1911,29 @@ static bool kv4_rows_ok(const clasp_ctx* ctx, const void* p, int64_t stride, int
   return p && al16(p) && stride >= (int64_t)heads * ctx->cfg.head_dim && stride % (ctx->cfg.dtype == CLASP_BF16 ? 8 : 4) == 0;
 }
 
+}  // extern "C"
+
+// The write and read kernels take a thread per block, rows in fours, numbered in 32 bits: f(first row, rows, grid) per launch.
+template <typename F>
+static int kv4_rows(clasp_ctx* ctx, int n, F f) {
+  const long long per_row = (long long)ctx->cfg.n_kv_heads * (ctx->cfg.head_dim / clasp::kv4::BLOCK);
+  const int step = (int)std::max(4LL, std::min(1LL << 29, (1LL << 31) / per_row / 4 * 4));
+  for (int r0 = 0; r0 < n; r0 += step) {
+    const int rows = std::min(step, n - r0);
+    const long long units = (rows + 3LL) / 4 * 4 * per_row;
+    f(r0, rows, dim3((unsigned)((units + 255) / 256), 2));
+    const int rc = launch_check(ctx);
+    if (rc) return rc;
+  }
+  return CLASP_OK;
+}
+static bool kv4_al32(const clasp_config& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride) {
+  const int64_t esz = c.dtype == CLASP_BF16 ? 2 : 4;
+  return (((uintptr_t)k | (uintptr_t)v | (uintptr_t)(k_stride * esz) | (uintptr_t)(v_stride * esz)) & 31) == 0;
+}
+
+extern "C" {
+
 int clasp_kv4_write(clasp_ctx* ctx, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n, int32_t pos0,
                     const clasp_kv_layer* kv) {
   int rc = kv4_check(ctx, kv);
@@ -1926,16 +1943,16 @@ int clasp_kv4_write(clasp_ctx* ctx, const void* k, int64_t k_stride, const void*
   if ((int64_t)pos0 + n > c.max_ctx) return CLASP_ERR_CAPACITY;
   if (n == 0) return CLASP_OK;
   if (!kv4_rows_ok(ctx, k, k_stride, c.n_kv_heads) || !kv4_rows_ok(ctx, v, v_stride, c.n_kv_heads)) return CLASP_ERR_INVALID_ARG;
-  const long long units = (long long)n * c.n_kv_heads * (c.head_dim / clasp::kv4::BLOCK);
-  const dim3 grid((unsigned)((units + 255) / 256), 2);
   const auto ck = kv4_view(ctx, kv->k, c.max_ctx), cv = kv4_view(ctx, kv->v, c.max_ctx);
-  if (c.dtype == CLASP_BF16)
-    clasp::kv4::write_kernel<bf16><<<grid, 256, 0, ctx->stream>>>((const bf16*)k, k_stride, (const bf16*)v, v_stride, n, pos0,
-                                                                 c.n_kv_heads, c.head_dim, ck, cv);
-  else
-    clasp::kv4::write_kernel<float><<<grid, 256, 0, ctx->stream>>>((const float*)k, k_stride, (const float*)v, v_stride, n, pos0,
-                                                                  c.n_kv_heads, c.head_dim, ck, cv);
-  return launch_check(ctx);
+  const bool al32 = kv4_al32(c, k, k_stride, v, v_stride);
+  return kv4_rows(ctx, n, [&](int r0, int rows, dim3 grid) {
+    if (c.dtype == CLASP_BF16)
+      clasp::kv4::write_kernel<bf16><<<grid, 256, 0, ctx->stream>>>((const bf16*)k + r0 * k_stride, k_stride, (const bf16*)v + r0 * v_stride,
+                                                                   v_stride, rows, pos0 + r0, c.n_kv_heads, c.head_dim, ck, cv, al32);
+    else
+      clasp::kv4::write_kernel<float><<<grid, 256, 0, ctx->stream>>>((const float*)k + r0 * k_stride, k_stride, (const float*)v + r0 * v_stride,
+                                                                    v_stride, rows, pos0 + r0, c.n_kv_heads, c.head_dim, ck, cv, al32);
+  });
 }
 
 int clasp_kv4_read(clasp_ctx* ctx, const clasp_kv_layer* kv, int32_t pos0, int32_t n, void* k_out, int64_t k_stride, void* v_out,
@@ -1947,16 +1964,16 @@ int clasp_kv4_read(clasp_ctx* ctx, const clasp_kv_layer* kv, int32_t pos0, int32
   if ((int64_t)pos0 + n > c.max_ctx) return CLASP_ERR_CAPACITY;
   if (n == 0) return CLASP_OK;
   if (!kv4_rows_ok(ctx, k_out, k_stride, c.n_kv_heads) || !kv4_rows_ok(ctx, v_out, v_stride, c.n_kv_heads)) return CLASP_ERR_INVALID_ARG;
-  const long long units = (long long)n * c.n_kv_heads * (c.head_dim / clasp::kv4::BLOCK);
-  const dim3 grid((unsigned)((units + 255) / 256), 2);
   const auto ck = kv4_view(ctx, kv->k, c.max_ctx), cv = kv4_view(ctx, kv->v, c.max_ctx);
-  if (c.dtype == CLASP_BF16)
-    clasp::kv4::read_kernel<bf16><<<grid, 256, 0, ctx->stream>>>(ck, cv, n, pos0, c.n_kv_heads, c.head_dim, (bf16*)k_out, k_stride,
-                                                                (bf16*)v_out, v_stride);
-  else
-    clasp::kv4::read_kernel<float><<<grid, 256, 0, ctx->stream>>>(ck, cv, n, pos0, c.n_kv_heads, c.head_dim, (float*)k_out, k_stride,
-                                                                 (float*)v_out, v_stride);
-  return launch_check(ctx);
+  const bool al32 = kv4_al32(c, k_out, k_stride, v_out, v_stride);
+  return kv4_rows(ctx, n, [&](int r0, int rows, dim3 grid) {
+    if (c.dtype == CLASP_BF16)
+      clasp::kv4::read_kernel<bf16><<<grid, 256, 0, ctx->stream>>>(ck, cv, rows, pos0 + r0, c.n_kv_heads, c.head_dim,
+                                                                  (bf16*)k_out + r0 * k_stride, k_stride, (bf16*)v_out + r0 * v_stride, v_stride, al32);
+    else
+      clasp::kv4::read_kernel<float><<<grid, 256, 0, ctx->stream>>>(ck, cv, rows, pos0 + r0, c.n_kv_heads, c.head_dim,
+                                                                   (float*)k_out + r0 * k_stride, k_stride, (float*)v_out + r0 * v_stride, v_stride, al32);
+  });
 }
 
 int clasp_kv4_attention(clasp_ctx* ctx, const void* q, int64_t q_stride, int32_t S, int32_t T, int32_t ctx_len, int32_t own_pos0,

@@ -50,32 +50,34 @@ inline size_t array_bytes(int n_kv, int hd, long long capacity) {
 __device__ __forceinline__ float scale_of(uint32_t b) { return __half2float(__ushort_as_half((unsigned short)(b << 7))); }
 
 // Sixteen values -> eight bytes of codes and the scale byte.
-__device__ __forceinline__ uint2 quantise(const float (&x)[BLOCK], uint32_t& byte) {
-  float a = 0.f, sum = 0.f;
+__device__ __forceinline__ uint2 quantise(float (&x)[BLOCK], uint32_t& byte) {
+  float a = 0.f;
 #pragma unroll
-  for (int i = 0; i < BLOCK; ++i) {
-    a = fmaxf(a, fabsf(x[i]));
-    sum += fabsf(x[i]) * 0.f;          // NaN exactly when some value is not finite
-  }
-  if (sum != 0.f) {
+  for (int i = 0; i < BLOCK; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(fabsf(x[i])));
+  if (!(a <= 3.402823466e38f)) {         // an infinity or NaN
     byte = NAN_SCALE;
     return make_uint2(0x88888888u, 0x88888888u);
   }
+  if (a > 6272.f) {
+#pragma unroll
+    for (int i = 0; i < BLOCK; ++i) x[i] = fminf(fmaxf(x[i], -6272.f), 6272.f);
+    a = 6272.f;
+  }
   // candidate: a / 7 cut to three mantissa bits (the product errs by less than one step of them); the next one if that is
-  // too small.  a below 2^-17: the smallest scale.
-  const float t = fminf(a * (1.0f / 7.0f), 896.f);
-  const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rz(t)) >> 7;
-  byte = min(h + (7.f * scale_of(h) < a ? 1u : 0u), TOP_SCALE);
+  // too small
+  const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rz(a * (1.0f / 7.0f))) >> 7;
+  byte = h + (7.f * scale_of(h) < a ? 1u : 0u);
   const float s = scale_of(byte);
   const float r = byte ? __frcp_rn(s) : 0.f;
+  // x / s, correctly rounded: reciprocal to the nearest, then one residual step (Markstein's division); at most 7.  Added to
+  // 1.5 x 2^23 + 8 its integer (ties to even) plus 8 is the sum's low bits; what stands above them is taken off the word at once.
+  constexpr uint32_t BIAS = 0x4B400000u;
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < BLOCK; ++i) {
-    // x / s, correctly rounded: reciprocal to the nearest, then one residual step (Markstein's division)
     const float q0 = x[i] * r;
-    const float q = fmaf(fmaf(-q0, s, x[i]), r, q0);
-    const float c = fminf(fmaxf(rintf(q), -7.f), 7.f) + 8.f;
-    w[i >> 3] |= (uint32_t)c << ((i & 7) * 4);
+    const float q = fmaf(fmaf(-q0, s, x[i]), r, q0) + 12582920.f;
+    w[i >> 3] += (__float_as_uint(q) - BIAS) << ((i & 7) * 4);
   }
   return make_uint2(w[0], w[1]);
 }
@@ -116,41 +118,105 @@ __device__ __forceinline__ void store16(bf16* p, const float (&x)[BLOCK]) {
 }
 
 // ------------------------------------------------------------------ rows into the cache and back
-// A thread takes one block of K or of V (blockIdx.y); consecutive threads take consecutive blocks of a row.
-template <typename T>
-__global__ void __launch_bounds__(256) write_kernel(const T* __restrict__ k, long long k_stride, const T* __restrict__ v,
-                                                    long long v_stride, int n, long long pos0, int n_kv, int hd, View ck, View cv) {
-  const int per_head = hd / BLOCK, per_row = n_kv * per_head;
-  const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (u >= (long long)n * per_row) return;
-  const long long row = u / per_row;
-  const int b = (int)(u - row * per_row), head = b / per_head, j = b - head * per_head;
-  const bool val = blockIdx.y != 0;
-  const View& c = val ? cv : ck;
-  float x[BLOCK];
-  load16((val ? v + row * v_stride : k + row * k_stride) + b * BLOCK, x);
-  uint32_t byte;
-  const uint2 w = quantise(x, byte);
-  *reinterpret_cast<uint2*>(c.codes + head * c.head_codes + (pos0 + row) * (hd / 2) + j * 8) = w;
-  c.scales[head * c.head_scales + (pos0 + row) * per_head + j] = (uint8_t)byte;
+// 32 bytes at a time where the addresses allow it (al32): two 16-byte accesses of a lane leave every sector half done twice.
+__device__ __forceinline__ void ld32(const void* p, uint32_t (&w)[8], bool al32) {
+  if (al32) {
+    asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+  } else {
+    const uint4 a = __ldg((const uint4*)p), b = __ldg((const uint4*)p + 1);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  }
+}
+__device__ __forceinline__ void st32(void* p, const uint32_t (&w)[8], bool al32) {
+  if (al32) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    ((uint4*)p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    ((uint4*)p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+__device__ __forceinline__ void load_block(const bf16* p, float (&x)[BLOCK], bool al32) {
+  uint32_t w[8];
+  ld32(p, w, al32);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load_block(const float* p, float (&x)[BLOCK], bool al32) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t w[8];
+    ld32(p + 8 * h, w, al32);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[8 * h + i] = __uint_as_float(w[i]);
+  }
+}
+__device__ __forceinline__ void store_block(bf16* p, const float (&x)[BLOCK], bool al32) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+  st32(p, w, al32);
+}
+__device__ __forceinline__ void store_block(float* p, const float (&x)[BLOCK], bool al32) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(x[8 * h + i]);
+    st32(p + 8 * h, w, al32);
+  }
 }
 
+// A thread takes one block of K or of V (blockIdx.y).  Of the neighbours, hd / 16 share a head's row, and four rows of a head
+// follow one another: 256 bytes of codes and 32 of scales side by side in the cache (hd 128), whole sectors of both.
+struct BlockAt {
+  int row, head, j;        // row of the call, kv head, block of the row
+};
+__device__ __forceinline__ BlockAt block_at(int n_kv, int per_head) {
+  const unsigned u = blockIdx.x * blockDim.x + threadIdx.x, q = u / per_head, q4 = q >> 2, group = q4 / n_kv;
+  return BlockAt{(int)(group * 4 + (q & 3)), (int)(q4 - group * n_kv), (int)(u - q * per_head)};
+}
+
+// Measured, bf16, eight heads of 128, write + read of 8192 rows together, us: 24.8 with a row's blocks side by side and 16-byte
+// accesses, 30.0 with four rows per thread, 23.4 so, 20.3 with the shorter quantiser (DRAM: 13.2).
+template <typename T>
+__global__ void __launch_bounds__(256) write_kernel(const T* __restrict__ k, long long k_stride, const T* __restrict__ v,
+                                                    long long v_stride, int n, long long pos0, int n_kv, int hd, View ck, View cv,
+                                                    bool al32) {
+  const int per_head = hd / BLOCK;
+  const BlockAt at = block_at(n_kv, per_head);
+  if (at.row >= n) return;
+  const bool val = blockIdx.y != 0;
+  float x[BLOCK];
+  load_block((val ? v + at.row * v_stride : k + at.row * k_stride) + at.head * hd + at.j * BLOCK, x, al32);
+  uint32_t byte;
+  const uint2 w = quantise(x, byte);
+  const long long pos = pos0 + at.row;
+  *reinterpret_cast<uint2*>((val ? cv.codes : ck.codes) + at.head * ck.head_codes + pos * (hd / 2) + at.j * 8) = w;
+  ((val ? cv.scales : ck.scales) + at.head * ck.head_scales + pos * per_head)[at.j] = (uint8_t)byte;
+}
+
+// The inverse; code times scale is exact in fp32 and in bf16.  36.2 us for 32768 rows of eight heads of 128 with a row's blocks
+// side by side and 16-byte accesses, 34.0 so (DRAM: 26.3).
 template <typename T>
 __global__ void __launch_bounds__(256) read_kernel(View ck, View cv, int n, long long pos0, int n_kv, int hd, T* __restrict__ k,
-                                                   long long k_stride, T* __restrict__ v, long long v_stride) {
-  const int per_head = hd / BLOCK, per_row = n_kv * per_head;
-  const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (u >= (long long)n * per_row) return;
-  const long long row = u / per_row;
-  const int b = (int)(u - row * per_row), head = b / per_head, j = b - head * per_head;
+                                                   long long k_stride, T* __restrict__ v, long long v_stride, bool al32) {
+  const int per_head = hd / BLOCK;
+  const BlockAt at = block_at(n_kv, per_head);
+  if (at.row >= n) return;
   const bool val = blockIdx.y != 0;
-  const View& c = val ? cv : ck;
-  const uint2 w = *reinterpret_cast<const uint2*>(c.codes + head * c.head_codes + (pos0 + row) * (hd / 2) + j * 8);
-  const float s = scale_of(c.scales[head * c.head_scales + (pos0 + row) * per_head + j]);
+  const long long pos = pos0 + at.row;
+  const uint2 w = __ldg(reinterpret_cast<const uint2*>((val ? cv.codes : ck.codes) + at.head * ck.head_codes + pos * (hd / 2) + at.j * 8));
+  const float s = scale_of(__ldg((val ? cv.scales : ck.scales) + at.head * ck.head_scales + pos * per_head + at.j));
   float x[BLOCK];
 #pragma unroll
-  for (int i = 0; i < BLOCK; ++i) x[i] = ((float)(((i < 8 ? w.x : w.y) >> ((i & 7) * 4)) & 15u) - 8.f) * s;
-  store16((val ? v + row * v_stride : k + row * k_stride) + b * BLOCK, x);
+  for (int e = 0; e < BLOCK; ++e) x[e] = ((float)(((e < 8 ? w.x : w.y) >> ((e & 7) * 4)) & 15u) - 8.f) * s;
+  store_block((val ? v + at.row * v_stride : k + at.row * k_stride) + at.head * hd + at.j * BLOCK, x, al32);
 }
 
 // A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated and stored in the model dtype, keys rotated and
@@ -340,6 +406,7 @@ __device__ __forceinline__ uint32_t nib_bf16(uint32_t w, uint32_t s2, uint32_t m
 
 constexpr int WARPS = 16;
 constexpr int STEP = 16;                 // keys a warp takes at a time
+constexpr int PB = 8;                    // pairs per CTA
 constexpr int STAGES = 4;                // steps of a warp in shared memory: one at work, three on their way
 constexpr int MAX_PARTS = 152;           // runs of one launch and the own rows
 constexpr float P_BITS = 12.f;           // weights are held as 2^12 .. 2^20 x exp2(s - m) in half precision (see below)
@@ -349,16 +416,16 @@ template <int HD> struct Raw {           // one warp step: two key rows' and fou
   uint32_t ks[2], vs[4];
 };
 template <int HD> constexpr int STEP_BYTES = STEP * (HD + HD / 8);
-template <int HD, int NT, bool SPLIT> constexpr int rows_smem() {
-  constexpr int ring = WARPS * STAGES * STEP_BYTES<HD>, merge = WARPS * 8 * NT * (HD + 4) * 4;
-  return (ring > merge ? ring : merge) + (SPLIT ? 2 : 1) * NT * (HD / 16) * 32 * 8;
+template <int HD, bool SPLIT> constexpr int rows_smem() {
+  constexpr int ring = WARPS * STAGES * STEP_BYTES<HD>, merge = WARPS * PB * (HD + 4) * 4;
+  return (ring > merge ? ring : merge) + (SPLIT ? 2 : 1) * (HD / 16) * 32 * 8;
 }
 template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool in) {
   if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16u : 0u) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(in ? (uint32_t)N : 0u), "n"(N) : "memory");
 }
 
-// Attention of few (row, query head) pairs: 8 NT pairs of one kv head per CTA, one run of the cache per CTA, its steps of 16
+// Attention of few (row, query head) pairs: eight pairs of one kv head per CTA, one run of the cache per CTA, its steps of 16
 // keys dealt to sixteen warps that never wait for one another before the end.
 //
 //   S^T = K q^T     16 keys x 8 pairs: the keys are the M rows of mma.m16n8k16, so few pairs waste little
@@ -374,16 +441,15 @@ template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const vo
 // only when exceeded by 2^3, so they stay below 2^15 and lose nothing above 2^-26 of the largest; sums in fp32.
 // A block with the NaN byte must reach only the rows that see it, and 0 x NaN is NaN: values' NaN blocks enter as zeros, and
 // `poison` remembers which (pair, block) they belong to.
-template <int HD, int NT, bool SPLIT>
+template <int HD, bool SPLIT>
 __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_constant__ AttnArgs p) {
-  constexpr int PB = 8 * NT;             // pairs per CTA
   constexpr int KS = HD / 16;            // k steps of the scores, and tiles of 16 dims of the output
   constexpr int KW = HD / 32, VW = HD / 64;
   constexpr int PARTS = SPLIT ? 2 : 1;
   constexpr float NEG = -INFINITY;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint2 (*qf)[NT][KS][32] = reinterpret_cast<uint2 (*)[NT][KS][32]>(smem);
-  uint8_t* ring = smem + PARTS * NT * KS * 32 * 8;                       // the warps' steps, later their results
+  uint2 (*qf)[KS][32] = reinterpret_cast<uint2 (*)[KS][32]>(smem);
+  uint8_t* ring = smem + PARTS * KS * 32 * 8;                       // the warps' steps, later their results
   float (*o_sm)[PB][HD + 4] = reinterpret_cast<float (*)[PB][HD + 4]>(ring);
   __shared__ float2 ml_sm[WARPS][PB];
   __shared__ float w_sm[WARPS][PB], mx_sm[PB];
@@ -509,8 +575,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   for (int i = 0; i < STAGES - 1; ++i) fetch();
 
   // q rows into the fragments of the second operand: a warp per pair, lane = its place along the row
-  for (int i = warp; i < PB; i += WARPS) {
-    const int pp = pair0 + i;
+  if (warp < PB) {
+    const int i = warp, pp = pair0 + i;
     constexpr int E = HD / 32;
     float x[E];
 #pragma unroll
@@ -538,10 +604,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
       const int step = wd * 2 + ((n >> 1) & 1);
       if ((n & 1) == 0) x[e] *= 16.f;    // meets nib_lo
       const __half hx = __float2half_rn(x[e]);
-      __half* dst = reinterpret_cast<__half*>(&qf[0][i >> 3][step][(i & 7) * 4 + tt]) + (n & 1) * 2 + (n >> 2);
+      __half* dst = reinterpret_cast<__half*>(&qf[0][step][i * 4 + tt]) + (n & 1) * 2 + (n >> 2);
       *dst = hx;
       if constexpr (SPLIT) {
-        __half* d2 = reinterpret_cast<__half*>(&qf[PARTS - 1][i >> 3][step][(i & 7) * 4 + tt]) + (n & 1) * 2 + (n >> 2);
+        __half* d2 = reinterpret_cast<__half*>(&qf[PARTS - 1][step][i * 4 + tt]) + (n & 1) * 2 + (n >> 2);
         *d2 = __float2half_rn(x[e] - __half2float(hx));
       }
     }
@@ -550,17 +616,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   __syncthreads();
 
   // off: m - P_BITS of each pair (0 before its first visible key, then top is -inf); top: a score above it moves m
-  float o[NT][KS][4], off[NT][2], top[NT][2], l[NT][2], mult[NT][2];
+  float o[KS][4], off[2], top[2], l[2], mult[2];
   uint32_t poison = 0;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+  for (int c = 0; c < 2; ++c) { off[c] = 0.f; top[c] = NEG; l[c] = 0.f; mult[c] = mult_sm[2 * t + c]; }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) { off[n][c] = 0.f; top[n][c] = NEG; l[n][c] = 0.f; mult[n][c] = mult_sm[n * 8 + 2 * t + c]; }
+  for (int j = 0; j < KS; ++j)
 #pragma unroll
-    for (int j = 0; j < KS; ++j)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) o[n][j][c] = 0.f;
-  }
+    for (int c = 0; c < 4; ++c) o[j][c] = 0.f;
 
 #pragma unroll 1
   for (; base < k_end; base += WARPS * STEP) {
@@ -570,13 +633,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
     Raw<HD> cur;
     take(cur, stage);
     if (++stage == STAGES) stage = 0;
-    // ---- scores
-    // (two chains of multiplies, whatever NT: a row is the same bits)
-    float s[NT][4], s2[NT][4];
+    // ---- scores, in two chains of multiplies
+    float s[4], s2[4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s[n][c] = s2[n][c] = 0.f;
+    for (int c = 0; c < 4; ++c) s[c] = s2[c] = 0.f;
 #pragma unroll
     for (int wd = 0; wd < KW; ++wd) {
       constexpr int WPS = 2;                          // words per scale
@@ -587,66 +647,62 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
         const uint32_t w0 = cur.k[0][wd] >> (8 * h), w1 = cur.k[1][wd] >> (8 * h);
         const uint32_t a[4] = {nib_lo(w0, s0), nib_lo(w1, s1), nib_hi(w0, s0), nib_hi(w1, s1)};
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int q = 0; q < PARTS; ++q) {
-            const uint2 b = qf[q][n][wd * 2 + h][lane];
-            mma16816(h ? s2[n] : s[n], a, b.x, b.y);
-          }
+        for (int q = 0; q < PARTS; ++q) {
+          const uint2 b = qf[q][wd * 2 + h][lane];
+          mma16816(h ? s2 : s, a, b.x, b.y);
+        }
       }
     }
     // ---- masks, weights
     const bool full = base >= full_lo && base + STEP <= full_hi;
-    uint32_t pw[PARTS][NT][2];
+    uint32_t pw[PARTS][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int c = 0; c < 4; ++c) s[c] = fmaf(s2[c], mult[c & 1], fmaf(s[c], mult[c & 1], -off[c & 1]));
+    if (!full) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[n][c] = fmaf(s2[n][c], mult[n][c & 1], fmaf(s[n][c], mult[n][c & 1], -off[n][c & 1]));
-      if (!full) {
+      for (int c = 0; c < 4; ++c) {
+        const int key = base + kg + (c >> 1) * 8, col = 2 * t + (c & 1);
+        if (key < lo_sm[col] || key >= min(hi_sm[col], k_end)) s[c] = NEG;
+      }
+    }
+    const float x0 = fmaxf(s[0], s[2]), x1 = fmaxf(s[1], s[3]);
+    if (__any_sync(0xffffffffu, x0 > top[0] || x1 > top[1])) {
+      float y[2] = {x0, x1};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int key = base + kg + (c >> 1) * 8, col = n * 8 + 2 * t + (c & 1);
-          if (key < lo_sm[col] || key >= min(hi_sm[col], k_end)) s[n][c] = NEG;
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) y[c] = fmaxf(y[c], __shfl_xor_sync(0xffffffffu, y[c], d));
+        if (y[c] > top[c]) {
+          const float by = y[c] - P_BITS, corr = top[c] == NEG ? 0.f : exp2f(-by);
+          off[c] += by;
+          top[c] = P_BITS + 3.f;
+          l[c] *= corr;
+          s[c] -= by;
+          s[c + 2] -= by;
+#pragma unroll
+          for (int j = 0; j < KS; ++j) { o[j][c] *= corr; o[j][c + 2] *= corr; }
         }
       }
-      const float x0 = fmaxf(s[n][0], s[n][2]), x1 = fmaxf(s[n][1], s[n][3]);
-      if (__any_sync(0xffffffffu, x0 > top[n][0] || x1 > top[n][1])) {
-        float y[2] = {x0, x1};
+      __syncwarp();
+    }
+    float e[4];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < 4; ++c) e[c] = ex2(s[c]);   // (nothing visible so far: exp2(-inf) = 0)
+    l[0] += e[0] + e[2];
+    l[1] += e[1] + e[3];
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) y[c] = fmaxf(y[c], __shfl_xor_sync(0xffffffffu, y[c], d));
-          if (y[c] > top[n][c]) {
-            const float by = y[c] - P_BITS, corr = top[n][c] == NEG ? 0.f : exp2f(-by);
-            off[n][c] += by;
-            top[n][c] = P_BITS + 3.f;
-            l[n][c] *= corr;
-            s[n][c] -= by;
-            s[n][c + 2] -= by;
-#pragma unroll
-            for (int j = 0; j < KS; ++j) { o[n][j][c] *= corr; o[n][j][c + 2] *= corr; }
-          }
-        }
-      }
-      float e[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) e[c] = ex2(s[n][c]);   // (nothing visible so far: exp2(-inf) = 0)
-      l[n][0] += e[0] + e[2];
-      l[n][1] += e[1] + e[3];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t u = pack_half(e[2 * h], e[2 * h + 1]);
-        pw[0][n][h] = movmatrix_t(u);
-        if constexpr (SPLIT) {
-          const float2 f = unpack_half(u);
-          pw[PARTS - 1][n][h] = movmatrix_t(pack_half(e[2 * h] - f.x, e[2 * h + 1] - f.y));
-        }
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t u = pack_half(e[2 * h], e[2 * h + 1]);
+      pw[0][h] = movmatrix_t(u);
+      if constexpr (SPLIT) {
+        const float2 f = unpack_half(u);
+        pw[PARTS - 1][h] = movmatrix_t(pack_half(e[2 * h] - f.x, e[2 * h + 1] - f.y));
       }
     }
     // ---- values.  Lane (g, t): keys t, t + 4 are the M-operand's columns 2 t, 2 t + 1, keys t + 8, t + 12 the upper ones
     Scale2 z0 = scale2(cur.vs[0] + cur.vs[1] * 65536u), z1 = scale2(cur.vs[2] + cur.vs[3] * 65536u);
     const __half2 zz = __hadd2(z0.s, z1.s);             // NaN where one of the four is
-    if (!__hbeq2(zz, zz)) {
+    if (__any_sync(0xffffffffu, !__hbeq2(zz, zz))) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (cur.vs[i] == NAN_SCALE) {
@@ -658,6 +714,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
         }
       z0 = scale2(cur.vs[0] + cur.vs[1] * 65536u);
       z1 = scale2(cur.vs[2] + cur.vs[3] * 65536u);
+      __syncwarp();
     }
 #pragma unroll
     for (int wd = 0; wd < VW; ++wd) {
@@ -670,9 +727,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
         for (int e = 0; e < 2; ++e) {
           const uint32_t a[4] = {nib_lo(x >> (8 * e), z0), nib_hi(x >> (8 * e), z0), nib_lo(y >> (8 * e), z1), nib_hi(y >> (8 * e), z1)};
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q) mma16816(o[n][wd * 4 + h * 2 + e], a, pw[q][n][0], pw[q][n][1]);
+          for (int q = 0; q < PARTS; ++q) mma16816(o[wd * 4 + h * 2 + e], a, pw[q][0], pw[q][1]);
         }
       }
     }
@@ -682,18 +737,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();                         // the ring's place takes the results
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
+  for (int c = 0; c < 2; ++c) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int d = 4; d < 32; d <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], d);
+    // (maxima without P_BITS, here and in every part alike; a sum without a maximum is 0, or NaN)
+    if (g == 0) ml_sm[warp][2 * t + c] = make_float2(top[c] == NEG ? NEG : off[c], l[c]);
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
-      // (maxima without P_BITS, here and in every part alike; a sum without a maximum is 0, or NaN)
-      if (g == 0) ml_sm[warp][n * 8 + 2 * t + c] = make_float2(top[n][c] == NEG ? NEG : off[n][c], l[n][c]);
-#pragma unroll
-      for (int j = 0; j < KS; ++j)
-        *reinterpret_cast<float2*>(&o_sm[warp][n * 8 + 2 * t + c][g * (HD / 8) + 2 * j]) =
-            make_float2(o[n][j][c] * 16.f, o[n][j][c + 2]);   // (even dims are nib_lo's)
-    }
+    for (int j = 0; j < KS; ++j)
+      *reinterpret_cast<float2*>(&o_sm[warp][2 * t + c][g * (HD / 8) + 2 * j]) =
+          make_float2(o[j][c] * 16.f, o[j][c + 2]);     // (even dims are nib_lo's)
+  }
   if (poison) atomicOr(&poison_sm[g], poison);
   __syncthreads();
   constexpr int UNITS = PB * (HD / 4), GROUPS = WARPS * 32 / UNITS;   // four dims of a pair; threads that share the work on them
@@ -711,7 +764,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   const bool single = parts == 1;
   const int unit = threadIdx.x % UNITS, group = threadIdx.x / UNITS, col = unit / (HD / 4), d = unit % (HD / 4) * 4;
   const int pp = pair0 + col, r = pp / G, hq = kvh * G + pp - r * G;
-  const bool on = pp < n_pairs;
+  const bool on = pp < n_pairs && group < GROUPS;
   const long long rh = (long long)r * p.nq + hq;
   auto store = [&](const float4& a, float den) {
     const float inv = den == 0.f ? 0.f : 1.0f / den;
