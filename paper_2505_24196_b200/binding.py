@@ -203,7 +203,10 @@ class Clasp:
         if nbytes == 0:
             raise ClaspError(-2, "clasp_workspace_bytes")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self._dev, self._stream_ptr = self.workspace.device, self.stream.cuda_stream
+        # what the calls on single tokens read each time
+        self._index, self._stream_ptr = self.workspace.get_device(), self.stream.cuda_stream
+        self._hd, self._nq, self._nkv = cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
+        self._like = torch.empty(0, dtype=self.dtype, device=self.workspace.device)
         handle = C.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.lib.clasp_create(C.byref(cfg), self.workspace.data_ptr(), nbytes,
@@ -318,25 +321,23 @@ class Clasp:
     # ---- cache held in 4 bits (contexts made with FLAG_KV4)
     def _head_rows(self, t: torch.Tensor, heads: int, what: str) -> int:
         """Stride in elements of rows [n, heads, head_dim] in the model dtype; the heads of a row are contiguous."""
-        hd = self.cfg.head_dim
-        shape = t.shape
-        if len(shape) != 3 or shape[1] != heads or shape[2] != hd or t.dtype != self.dtype or t.device != self._dev:
-            raise ValueError(f"{what}: [n, {heads}, {hd}] {self.dtype} on {self._dev} expected")
+        shape, hd = t.shape, self._hd
+        if len(shape) != 3 or shape[1] != heads or shape[2] != hd or t.dtype is not self.dtype or t.get_device() != self._index:
+            raise ValueError(f"{what}: [n, {heads}, {hd}] {self.dtype} on {self.workspace.device} expected")
         sr, sh, sd = t.stride()
         if (sd != 1 or (sh != hd and heads > 1)) and shape[0]:
             raise ValueError(f"{what}: the heads of a row must be contiguous")
         return sr if shape[0] > 1 else max(sr, heads * hd)
 
-    def _new_rows(self, *shape: int) -> torch.Tensor:
-        t = torch.empty(shape, dtype=self.dtype, device=self._dev)
+    def _new_rows(self, t: torch.Tensor) -> torch.Tensor:
         # memory handed out for another stream than the one that fills it
-        if torch._C._cuda_getCurrentRawStream(self._dev.index) != self._stream_ptr:
+        if torch._C._cuda_getCurrentRawStream(self._index) != self._stream_ptr:
             t.record_stream(self.stream)
         return t
 
     @staticmethod
     def _kv4_layer(kv: KV4Cache, layer: int):
-        if not isinstance(kv, KV4Cache):
+        if type(kv) is not KV4Cache and not isinstance(kv, KV4Cache):
             raise ValueError("a KV4Cache is needed")
         if not 0 <= layer < len(kv.layers):
             raise ValueError(f"no layer {layer}")
@@ -344,7 +345,7 @@ class Clasp:
 
     def kv4_write(self, k: torch.Tensor, v: torch.Tensor, pos0: int, kv: KV4Cache, layer: int = 0):
         """Quantise rows k, v [n, n_kv_heads, head_dim] into positions pos0.. of one layer of a 4-bit cache."""
-        h = self.cfg.n_kv_heads
+        h = self._nkv
         ks, vs = self._head_rows(k, h, "k"), self._head_rows(v, h, "v")
         n = k.shape[0]
         if v.shape[0] != n:
@@ -355,15 +356,16 @@ class Clasp:
     def kv4_read(self, pos0: int, n: int, kv: KV4Cache, layer: int = 0, k_out: Optional[torch.Tensor] = None,
                  v_out: Optional[torch.Tensor] = None):
         """Rows pos0..pos0+n-1 of one layer of a 4-bit cache in the model dtype: (k, v), each [n, n_kv_heads, head_dim]."""
-        h = self.cfg.n_kv_heads
+        h = self._nkv
         if n < 0:
             raise ValueError("n: a number of rows")
         if k_out is None and v_out is None:
-            k_out, v_out = self._new_rows(2, n, h, self.cfg.head_dim).unbind(0)
-            ks = vs = h * self.cfg.head_dim
+            shape = (n, h, self._hd)
+            k_out, v_out = self._new_rows(self._like.new_empty(shape)), self._new_rows(self._like.new_empty(shape))
+            ks = vs = h * self._hd
         else:
-            k_out = self._new_rows(n, h, self.cfg.head_dim) if k_out is None else k_out
-            v_out = self._new_rows(n, h, self.cfg.head_dim) if v_out is None else v_out
+            k_out = self._new_rows(self._like.new_empty((n, h, self._hd))) if k_out is None else k_out
+            v_out = self._new_rows(self._like.new_empty((n, h, self._hd))) if v_out is None else v_out
             ks, vs = self._head_rows(k_out, h, "k_out"), self._head_rows(v_out, h, "v_out")
             if k_out.shape[0] != n or v_out.shape[0] != n:
                 raise ValueError("k_out, v_out: n rows")
@@ -377,7 +379,7 @@ class Clasp:
         cache.  Every row sees positions [0, ctx_len) -- with `visible` (int32 [S*T], device) row r only [0, visible[r]) of them
         -- and, with own_pos0, the rows of its own state up to itself, whose keys and values lie at positions own_pos0 + row.  A
         row that sees nothing gives zeros.  `out` must not overlap q."""
-        h = self.cfg.n_q_heads
+        h = self._nq
         qs = self._head_rows(q, h, "q")
         R = q.shape[0]
         if T < 1 or R % T:
@@ -390,7 +392,7 @@ class Clasp:
         elif own_pos0 < 0:
             raise ValueError("own_pos0: a position")
         if out is None:
-            out, os = self._new_rows(R, h, self.cfg.head_dim), h * self.cfg.head_dim
+            out, os = self._new_rows(torch.empty_like(q)), h * self._hd    # (rows with gaps give rows without)
         else:
             os = self._head_rows(out, h, "out")
             if out.shape[0] != R:

@@ -628,7 +628,17 @@ int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
   k4::attn_many_kernel<HD, NB><<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
   int rc = launch_check(ctx);
   if (rc || p.splits == 1) return rc;
-  k4::merge_kernel<HD, NB><<<items * (HD / 4) * NB / 2, 256, 0, ctx->stream>>>(p);
+  // its launch overlaps the attention's end (the kernel itself waits for it): 12 states over 8192 positions MERGE_US us
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(items * (HD / 4) * NB / 2);
+  lc.blockDim = dim3(256);
+  lc.stream = ctx->stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = &attr;
+  lc.numAttrs = 1;
+  CUDA_TRY(cudaLaunchKernelEx(&lc, k4::merge_kernel<HD, NB>, p));
   return launch_check(ctx);
 }
 
@@ -1410,19 +1420,20 @@ int clasp_create(const clasp_config* cfg, void* workspace, size_t workspace_byte
   int dev = 0, n_dev = 0;
   if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev < 1) return CLASP_ERR_CUDA;
   CUDA_TRY(cudaGetDevice(&dev));
-  cudaDeviceProp prop;
-  CUDA_TRY(cudaGetDeviceProperties(&prop, dev));
+  int n_sms = 0, major = 0;
+  CUDA_TRY(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev));
+  CUDA_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
   clasp_ctx* ctx = new clasp_ctx();
   ctx->cfg = *cfg;
   ctx->stream = (cudaStream_t)cuda_stream;
   ctx->ws = ws;
   ctx->layers.resize(cfg->L);
   ctx->loaded.assign(cfg->L, 0);
-  ctx->num_sms = prop.multiProcessorCount;
+  ctx->num_sms = n_sms;
   ctx->device = dev;
   ctx->use_tc = cfg->dtype == CLASP_BF16 && !(cfg->flags & CLASP_FLAG_FORCE_SIMT);
   if (ctx->use_tc) {
-    if (prop.major != 10) {  // the tcgen05 kernel exists for sm_100a only
+    if (major != 10) {  // the tcgen05 kernel exists for sm_100a only
       delete ctx;
       return CLASP_ERR_CUDA;
     }

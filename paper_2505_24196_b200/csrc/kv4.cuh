@@ -904,6 +904,7 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
     if (threadIdx.x == 0) atomicExch(p.status, 1);
     return;
   }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (merge_kernel, which waits for this grid's end)
   if (threadIdx.x == 0) {
     for (int s = 0; s < RING; ++s) {
       tc::mbar_init(tc::smem_u32(&sh->full[s]), 4);
@@ -1107,32 +1108,29 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
       const int j = threadIdx.x % LPR;
       int qrow = (int)threadIdx.x / LPR, rr = (pair0 + qrow) / Gq, hh = (pair0 + qrow) - rr * Gq;
       const int dr = STEP_ROWS / Gq, dh = STEP_ROWS - dr * Gq;
-#pragma unroll 1
-      for (int e0 = 0; e0 < LPR; e0 += 4) {   // four rows' loads are in flight at a time
-        uint4 w[4][2];
+      uint4 w[LPR][2];                        // all loads in flight at once
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          w[e][0] = w[e][1] = make_uint4(0, 0, 0, 0);
-          if (rr < p.R) {
-            const uint4* src = reinterpret_cast<const uint4*>((const bf16*)p.q + (long long)rr * p.q_stride +
-                                                              (long long)(kvh * Gq + hh) * HD + j * 16);
-            w[e][0] = src[0];
-            w[e][1] = src[1];
-          }
-          rr += dr;
-          hh += dh;
-          if (hh >= Gq) { hh -= Gq; ++rr; }
+      for (int e = 0; e < LPR; ++e) {
+        w[e][0] = w[e][1] = make_uint4(0, 0, 0, 0);
+        if (rr < p.R) {
+          const uint4* src = reinterpret_cast<const uint4*>((const bf16*)p.q + (long long)rr * p.q_stride +
+                                                            (long long)(kvh * Gq + hh) * HD + j * 16);
+          w[e][0] = src[0];
+          w[e][1] = src[1];
         }
+        rr += dr;
+        hh += dh;
+        if (hh >= Gq) { hh -= Gq; ++rr; }
+      }
 #pragma unroll
-        for (int e = 0; e < 4; ++e, qrow += STEP_ROWS) {
-          uint8_t* dst = smem + (qrow / TP) * Q_BYTES + (j >> 2) * HALF_Q + (qrow % TP) * 128;
+      for (int e = 0; e < LPR; ++e, qrow += STEP_ROWS) {
+        uint8_t* dst = smem + (qrow / TP) * Q_BYTES + (j >> 2) * HALF_Q + (qrow % TP) * 128;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {       // the order of the codes' conversion: dims 0 4, 1 5, 2 6, 3 7 of each eight
-            const uint4 u = w[e][h];
-            *reinterpret_cast<uint4*>(dst + ((((j & 3) * 2 + h) ^ (qrow & 7)) << 4)) =
-                make_uint4(__byte_perm(u.x, u.z, 0x5410), __byte_perm(u.x, u.z, 0x7632), __byte_perm(u.y, u.w, 0x5410),
-                           __byte_perm(u.y, u.w, 0x7632));
-          }
+        for (int h = 0; h < 2; ++h) {         // the order of the codes' conversion: dims 0 4, 1 5, 2 6, 3 7 of each eight
+          const uint4 u = w[e][h];
+          *reinterpret_cast<uint4*>(dst + ((((j & 3) * 2 + h) ^ (qrow & 7)) << 4)) =
+              make_uint4(__byte_perm(u.x, u.z, 0x5410), __byte_perm(u.x, u.z, 0x7632), __byte_perm(u.y, u.w, 0x5410),
+                         __byte_perm(u.y, u.w, 0x7632));
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1317,6 +1315,7 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Attn
   const int item = blockIdx.x / PER, chunk = blockIdx.x % PER * CHUNKS + (int)threadIdx.x / PAIRS;
   const int pair = threadIdx.x % PAIRS, Gq = p.nq / p.nkv;
   const int kvh = item % p.nkv, pp = (p.blocks - 1 - item / p.nkv) * PAIRS + pair;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // (launched while the parts are still being made)
   if (pp >= p.R * Gq) return;
   const float2* ml = p.part_ml + (long long)item * p.splits * PAIRS + pair;
   const float* src = p.part + ((long long)item * p.splits * HD + chunk * 4) * PAIRS + pair;
