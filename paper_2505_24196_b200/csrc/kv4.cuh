@@ -118,6 +118,20 @@ __device__ __forceinline__ void store16(bf16* p, const float (&x)[BLOCK]) {
 }
 
 // ------------------------------------------------------------------ rows into the cache and back
+// lanes of a 32-bit logic operation: (x & m) | o
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t o) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(m), "r"(o));
+  return y;
+}
+// Two codes, the low four bits of each half, as bf16 values (c - 8) s: four low mantissa bits of 128 make 128 + c without an integer
+// conversion, then (128 + c) s - 136 s in one step, exact (136 s has 8 significant bits).  s2, m136: s and -136 s in both halves.
+__device__ __forceinline__ uint32_t nib_bf16(uint32_t w, uint32_t s2, uint32_t m136) {
+  uint32_t y;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(and_or(w, 0x000F000Fu, 0x43004300u)), "r"(s2), "r"(m136));
+  return y;
+}
+
 // 32 bytes at a time where the addresses allow it (al32): two 16-byte accesses of a lane leave every sector half done twice.
 __device__ __forceinline__ void ld32(const void* p, uint32_t (&w)[8], bool al32) {
   if (al32) {
@@ -156,12 +170,6 @@ __device__ __forceinline__ void load_block(const float* p, float (&x)[BLOCK], bo
     for (int i = 0; i < 8; ++i) x[8 * h + i] = __uint_as_float(w[i]);
   }
 }
-__device__ __forceinline__ void store_block(bf16* p, const float (&x)[BLOCK], bool al32) {
-  uint32_t w[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-  st32(p, w, al32);
-}
 __device__ __forceinline__ void store_block(float* p, const float (&x)[BLOCK], bool al32) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -172,51 +180,61 @@ __device__ __forceinline__ void store_block(float* p, const float (&x)[BLOCK], b
   }
 }
 
-// A thread takes one block of K or of V (blockIdx.y).  Of the neighbours, hd / 16 share a head's row, and four rows of a head
-// follow one another: 256 bytes of codes and 32 of scales side by side in the cache (hd 128), whole sectors of both.
-struct BlockAt {
-  int row, head, j;        // row of the call, kv head, block of the row
-};
-__device__ __forceinline__ BlockAt block_at(int n_kv, int per_head) {
-  const unsigned u = blockIdx.x * blockDim.x + threadIdx.x, q = u / per_head, q4 = q >> 2, group = q4 / n_kv;
-  return BlockAt{(int)(group * 4 + (q & 3)), (int)(q4 - group * n_kv), (int)(u - q * per_head)};
-}
-
-// Measured, bf16, eight heads of 128, write + read of 8192 rows together, us: 24.8 with a row's blocks side by side and 16-byte
-// accesses, 30.0 with four rows per thread, 23.4 so, 20.3 with the shorter quantiser (DRAM: 13.2).
-template <typename T>
+// A CTA takes one kv head of K or of V (blockIdx.y), a thread one block.  Neighbours take the blocks of a row, then of the next
+// row: a warp's codes and scales lie side by side in the cache, whole sectors of both.
+//
+// Measured, bf16, eight heads of 128, write + read of 8192 rows together, us: 24.8 with the heads of a row side by side and 16-byte
+// accesses, 30.0 with four rows per thread, 23.4 so, 20.3 with the shorter quantiser, 15.7 without divisions (DRAM: 13.2).
+template <typename T, int HD>
 __global__ void __launch_bounds__(256) write_kernel(const T* __restrict__ k, long long k_stride, const T* __restrict__ v,
-                                                    long long v_stride, int n, long long pos0, int n_kv, int hd, View ck, View cv,
-                                                    bool al32) {
-  const int per_head = hd / BLOCK;
-  const BlockAt at = block_at(n_kv, per_head);
-  if (at.row >= n) return;
-  const bool val = blockIdx.y != 0;
+                                                    long long v_stride, int n, long long pos0, View ck, View cv, bool al32) {
+  constexpr int PER = HD / BLOCK;
+  const unsigned u = blockIdx.x * 256u + threadIdx.x, j = u % PER;
+  const int row = (int)(u / PER), head = blockIdx.y >> 1;
+  if (row >= n) return;
+  const bool val = blockIdx.y & 1;
   float x[BLOCK];
-  load_block((val ? v + at.row * v_stride : k + at.row * k_stride) + at.head * hd + at.j * BLOCK, x, al32);
+  load_block((val ? v + row * v_stride : k + row * k_stride) + head * HD + j * BLOCK, x, al32);
   uint32_t byte;
   const uint2 w = quantise(x, byte);
-  const long long pos = pos0 + at.row;
-  *reinterpret_cast<uint2*>((val ? cv.codes : ck.codes) + at.head * ck.head_codes + pos * (hd / 2) + at.j * 8) = w;
-  ((val ? cv.scales : ck.scales) + at.head * ck.head_scales + pos * per_head)[at.j] = (uint8_t)byte;
+  const long long at = (pos0 + row) * PER + j;
+  *reinterpret_cast<uint2*>((val ? cv.codes : ck.codes) + head * ck.head_codes + at * 8) = w;
+  ((val ? cv.scales : ck.scales) + head * ck.head_scales)[at] = (uint8_t)byte;
 }
 
-// The inverse; code times scale is exact in fp32 and in bf16.  36.2 us for 32768 rows of eight heads of 128 with a row's blocks
-// side by side and 16-byte accesses, 34.0 so (DRAM: 26.3).
-template <typename T>
-__global__ void __launch_bounds__(256) read_kernel(View ck, View cv, int n, long long pos0, int n_kv, int hd, T* __restrict__ k,
-                                                   long long k_stride, T* __restrict__ v, long long v_stride, bool al32) {
-  const int per_head = hd / BLOCK;
-  const BlockAt at = block_at(n_kv, per_head);
-  if (at.row >= n) return;
-  const bool val = blockIdx.y != 0;
-  const long long pos = pos0 + at.row;
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>((val ? cv.codes : ck.codes) + at.head * ck.head_codes + pos * (hd / 2) + at.j * 8));
-  const float s = scale_of(__ldg((val ? cv.scales : ck.scales) + at.head * ck.head_scales + pos * per_head + at.j));
-  float x[BLOCK];
+// The inverse; code times scale is exact in fp32 and in bf16.  36.2 us for 32768 rows of eight heads of 128 with the heads of a
+// row side by side and 16-byte accesses, 34.0 in whole sectors, 31.8 without divisions and with paired conversions (DRAM: 26.3).
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) read_kernel(View ck, View cv, int n, long long pos0, T* __restrict__ k, long long k_stride,
+                                                   T* __restrict__ v, long long v_stride, bool al32) {
+  constexpr int PER = HD / BLOCK;
+  const unsigned u = blockIdx.x * 256u + threadIdx.x, j = u % PER;
+  const int row = (int)(u / PER), head = blockIdx.y >> 1;
+  if (row >= n) return;
+  const bool val = blockIdx.y & 1;
+  const long long at = (pos0 + row) * PER + j;
+  const uint2 w = __ldg(reinterpret_cast<const uint2*>((val ? cv.codes : ck.codes) + head * ck.head_codes + at * 8));
+  const float s = scale_of(__ldg((val ? cv.scales : ck.scales) + head * ck.head_scales + at));
+  T* dst = (val ? v + row * v_stride : k + row * k_stride) + head * HD + j * BLOCK;
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t sc = pack_bf16(s, s), off = pack_bf16(s * -136.f, s * -136.f);
+    uint32_t y[8];
 #pragma unroll
-  for (int e = 0; e < BLOCK; ++e) x[e] = ((float)(((e < 8 ? w.x : w.y) >> ((e & 7) * 4)) & 15u) - 8.f) * s;
-  store_block((val ? v + at.row * v_stride : k + at.row * k_stride) + at.head * hd + at.j * BLOCK, x, al32);
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t c = h ? w.y : w.x;
+      const uint32_t a = nib_bf16(c, sc, off), b = nib_bf16(c >> 4, sc, off), d = nib_bf16(c >> 8, sc, off), e = nib_bf16(c >> 12, sc, off);
+      y[4 * h] = __byte_perm(a, b, 0x5410);        // values 0 1, 2 3, 4 5, 6 7 from 0 4, 1 5, 2 6, 3 7
+      y[4 * h + 1] = __byte_perm(d, e, 0x5410);
+      y[4 * h + 2] = __byte_perm(a, b, 0x7632);
+      y[4 * h + 3] = __byte_perm(d, e, 0x7632);
+    }
+    st32(dst, y, al32);
+  } else {
+    float x[BLOCK];
+#pragma unroll
+    for (int e = 0; e < BLOCK; ++e) x[e] = ((float)(((e < 8 ? w.x : w.y) >> ((e & 7) * 4)) & 15u) - 8.f) * s;
+    store_block(dst, x, al32);
+  }
 }
 
 // A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated and stored in the model dtype, keys rotated and
@@ -317,13 +335,6 @@ __device__ __forceinline__ float ex2(float x) {
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
 __device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
-// lanes of a 32-bit logic operation: (x & m) | o
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t o) {
-  uint32_t y;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(m), "r"(o));
-  return y;
-}
-
 // A query row for half precision: the power of two that brings its largest magnitude into [2^9, 2^10), and
 // the factor that takes it back and brings the scores into units of log2 (1 / sqrt(hd) aside).  LANES neighbouring lanes hold a row,
 // N values each.  A row with an infinity or NaN in it has no finite score: its factor is NaN, and so are all its weights.
@@ -394,14 +405,6 @@ __device__ __forceinline__ uint32_t nib_lo(uint32_t w, const Scale2& s) {
 }
 __device__ __forceinline__ uint32_t nib_hi(uint32_t w, const Scale2& s) {
   return as_u32(__hfma2(as_half2(and_or(w, 0x00F000F0u, 0x64006400u)), s.s16, s.m72));
-}
-
-// The same values as bf16, one nibble at a time from the low four bits of each half: 128 + c, then (128 + c) s - 136 s in one
-// step, exact as well (136 s has 8 significant bits).
-__device__ __forceinline__ uint32_t nib_bf16(uint32_t w, uint32_t s2, uint32_t m136) {
-  uint32_t y;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(and_or(w, 0x000F000Fu, 0x43004300u)), "r"(s2), "r"(m136));
-  return y;
 }
 
 constexpr int WARPS = 16;
