@@ -186,6 +186,7 @@ class KV4Cache:
             self.array[l].k = self.k[l].data_ptr()
             self.array[l].v = self.v[l].data_ptr()
         self.layers = [C.pointer(self.array[l]) for l in range(cfg.L)]
+        self.layout = (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim)
 
 
 class Clasp:
@@ -205,6 +206,7 @@ class Clasp:
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         # what the calls on single tokens read each time
         self._index, self._stream_ptr = self.workspace.get_device(), self.stream.cuda_stream
+        self._kv4, self._layout = bool(cfg.flags & FLAG_KV4), (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim)
         self._hd, self._nq, self._nkv = cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
         self._like = torch.empty(0, dtype=self.dtype, device=self.workspace.device)
         handle = C.c_void_p()
@@ -241,6 +243,15 @@ class Clasp:
         _check(self.lib.clasp_load_head(self.handle, head["embed"].data_ptr(), head["final_norm"].data_ptr(),
                                         head["lm_head"].data_ptr()), "clasp_load_head")
 
+    def _array(self, kv):
+        """The layers of a cache of the kind and layout this context was made for: a packed cache in place of a plain one, or one
+        of another capacity, would be read and written past its end."""
+        if isinstance(kv, KV4Cache) != self._kv4:
+            raise ValueError("contexts made with FLAG_KV4 take a KV4Cache, others a KVCache")
+        if self._kv4 and kv.layout != self._layout:
+            raise ValueError(f"cache of (layers, positions, kv heads, head_dim) {kv.layout}, context of {self._layout}")
+        return kv.array
+
     # ---- the calls of the hot path
     def dp_search(self, hidden_states: torch.Tensor, layer_stride: int, token_stride: int, kv: KVCache,
                   ctx_len: int, pos0: int, T: int, M: int, want_margins=True, want_g=True,
@@ -254,7 +265,7 @@ class Clasp:
         margins = torch.empty((L + 1, M + 1), dtype=torch.float32, device=dev) if want_margins else None
         g = torch.empty((T, d), dtype=torch.float32, device=dev) if want_g else None
         _check(self.lib.clasp_dp_search(self.handle, hidden_states.data_ptr(), layer_stride, token_stride,
-                                        kv.array, ctx_len, pos0, T, M, mask.data_ptr(), scores.data_ptr(),
+                                        self._array(kv), ctx_len, pos0, T, M, mask.data_ptr(), scores.data_ptr(),
                                         _ptr(margins), _ptr(g), _ptr(forced_choice)), "clasp_dp_search")
         return {"S": mask, "D": scores, "margin": margins, "g_final": g}
 
@@ -267,26 +278,26 @@ class Clasp:
             argmax_out = torch.empty(max(n_head_rows, 1), dtype=torch.int32, device=self.device)
         if want_hidden and hidden_out is None:
             hidden_out = torch.empty((n, L + 1, d), dtype=torch.float32, device=self.device)
-        _check(self.lib.clasp_verify(self.handle, tokens.data_ptr(), n, pos0, kv.array, n_head_rows,
+        _check(self.lib.clasp_verify(self.handle, tokens.data_ptr(), n, pos0, self._array(kv), n_head_rows,
                                      argmax_out.data_ptr(), _ptr(hidden_out) if want_hidden else None),
                "clasp_verify")
         return argmax_out[:n_head_rows], hidden_out
 
     def draft_forward(self, skip_mask_host: bytes, token_in: torch.Tensor, pos: int, kv: KVCache,
                       token_out: torch.Tensor, top1_prob_out: Optional[torch.Tensor] = None):
-        _check(self.lib.clasp_draft_forward(self.handle, skip_mask_host, token_in.data_ptr(), pos, kv.array,
+        _check(self.lib.clasp_draft_forward(self.handle, skip_mask_host, token_in.data_ptr(), pos, self._array(kv),
                                             token_out.data_ptr(), _ptr(top1_prob_out)), "clasp_draft_forward")
 
     def draft_sample(self, skip_mask_host: bytes, token_in: torch.Tensor, pos: int, kv: KVCache, temperature: float,
                      seed: int, rnd: int, token_out: torch.Tensor, logits_out: torch.Tensor):
-        _check(self.lib.clasp_draft_sample(self.handle, skip_mask_host, token_in.data_ptr(), pos, kv.array, temperature,
+        _check(self.lib.clasp_draft_sample(self.handle, skip_mask_host, token_in.data_ptr(), pos, self._array(kv), temperature,
                                            seed, rnd, token_out.data_ptr(), logits_out.data_ptr()), "clasp_draft_sample")
 
     def verify_sample(self, tokens: torch.Tensor, pos0: int, kv: KVCache, n_drafts: int,
                       draft_logits: Optional[torch.Tensor], temperature: float, seed: int, rnd: int,
                       logits_ws: torch.Tensor, n_accepted_out: torch.Tensor, committed_out: torch.Tensor,
                       hidden_out: Optional[torch.Tensor] = None):
-        _check(self.lib.clasp_verify_sample(self.handle, tokens.data_ptr(), tokens.numel(), pos0, kv.array, n_drafts,
+        _check(self.lib.clasp_verify_sample(self.handle, tokens.data_ptr(), tokens.numel(), pos0, self._array(kv), n_drafts,
                                             _ptr(draft_logits), temperature, seed, rnd, logits_ws.data_ptr(),
                                             n_accepted_out.data_ptr(), committed_out.data_ptr(), _ptr(hidden_out)),
                "clasp_verify_sample")
@@ -304,7 +315,8 @@ class Clasp:
                       kv: KVCache, write_kv: bool = False) -> torch.Tensor:
         assert x_in.dtype == torch.float32 and x_in.is_contiguous() and x_in.shape == (S * T, self.cfg.d_model)
         out = torch.empty_like(x_in)
-        kvl = ClaspKvLayer(kv.array[layer].k, kv.array[layer].v)
+        arr = self._array(kv)
+        kvl = ClaspKvLayer(arr[layer].k, arr[layer].v)
         _check(self.lib.clasp_layer_forward(self.handle, layer, x_in.data_ptr(), x_in.shape[1], S, T, ctx_len,
                                             pos0, C.byref(kvl), int(write_kv), out.data_ptr(), out.shape[1]),
                "clasp_layer_forward")
@@ -335,13 +347,17 @@ class Clasp:
             t.record_stream(self.stream)
         return t
 
-    @staticmethod
-    def _kv4_layer(kv: KV4Cache, layer: int):
-        if type(kv) is not KV4Cache and not isinstance(kv, KV4Cache):
-            raise ValueError("a KV4Cache is needed")
+    def _kv4_layer(self, kv: KV4Cache, layer: int):
+        if type(kv) is not KV4Cache and not isinstance(kv, KV4Cache) or kv.layout != self._layout:
+            raise ValueError("a KV4Cache of this context's layout is needed")
         if not 0 <= layer < len(kv.layers):
             raise ValueError(f"no layer {layer}")
         return kv.layers[layer]
+
+    def _positions(self, *at: int):
+        for v in at:                    # (the library's numbers have 32 bits: larger ones would come round)
+            if not -1 <= v <= 1 << 30:
+                raise ValueError(f"{v}: not a position or a number of rows")
 
     def kv4_write(self, k: torch.Tensor, v: torch.Tensor, pos0: int, kv: KV4Cache, layer: int = 0):
         """Quantise rows k, v [n, n_kv_heads, head_dim] into positions pos0.. of one layer of a 4-bit cache."""
@@ -350,6 +366,7 @@ class Clasp:
         n = k.shape[0]
         if v.shape[0] != n:
             raise ValueError("k and v: as many rows")
+        self._positions(pos0)
         _check(self.lib.clasp_kv4_write(self.handle, k.data_ptr(), ks, v.data_ptr(), vs, n, pos0, self._kv4_layer(kv, layer)),
                "clasp_kv4_write")
 
@@ -359,6 +376,7 @@ class Clasp:
         h = self._nkv
         if n < 0:
             raise ValueError("n: a number of rows")
+        self._positions(pos0, n)
         if k_out is None and v_out is None:
             shape = (n, h, self._hd)
             k_out, v_out = self._new_rows(self._like.new_empty(shape)), self._new_rows(self._like.new_empty(shape))
@@ -391,6 +409,7 @@ class Clasp:
             own_pos0 = -1
         elif own_pos0 < 0:
             raise ValueError("own_pos0: a position")
+        self._positions(ctx_len, own_pos0)
         if out is None:
             out, os = self._new_rows(torch.empty_like(q)), h * self._hd    # (rows with gaps give rows without)
         else:

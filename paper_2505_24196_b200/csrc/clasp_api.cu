@@ -45,6 +45,7 @@ constexpr int KV4_MAX_HEADS = 1 << 14; // kv heads of such a model (grids)
 constexpr int KV4_ROWS = 64;           // rows per launch of the attention of few rows: bounds its workspace
 constexpr int KV4_MIN_STEPS = 4;       // steps a warp takes in a full run at least: joining two runs costs about as much
 constexpr int KV4_FEW_ROWS = 16;       // rows of a call (bf16) whose sums do not depend on how many share it
+constexpr int KV4_FEW_PAIRS = 16;      // (row, query head) pairs per kv head from which candidate states take the tensor cores
 constexpr size_t KV4_MANY_SLOTS = 160 * 256;   // (pair, part) slots of the attention of many rows: about one CTA's pairs per SM
 constexpr int MAX_COUNTERS = 4096;   // tiles of one GEMM launch that may use split-K
 constexpr size_t PARTIAL_FLOATS = (size_t)296 * 2 * 128 * 128 + (1 << 20);
@@ -169,8 +170,11 @@ Workspace carve(const clasp_config& c, uint8_t* base) {
   w.rope = (float2*)take(R * (c.head_dim / 2) * sizeof(float2));
   const size_t att_chunks = clasp::ATT_MAX_CACHE_CHUNKS + (R + clasp::ATT_KEYS - 1) / clasp::ATT_KEYS;
   if (is_kv4(c)) {
-    const size_t slots = std::max(std::min(R, (size_t)(c.dtype == CLASP_BF16 && !(c.flags & CLASP_FLAG_FORCE_SIMT) ? KV4_FEW_ROWS : KV4_ROWS)) *
-                                      c.n_q_heads * kv4_max_parts(c), KV4_MANY_SLOTS);
+    const bool tc = c.dtype == CLASP_BF16 && !(c.flags & CLASP_FLAG_FORCE_SIMT);
+    const size_t few = std::min(R, (size_t)(tc ? KV4_FEW_ROWS : KV4_ROWS)) * c.n_q_heads * kv4_max_parts(c);
+    // the tensor-core attention takes calls of more than KV4_FEW_ROWS rows or KV4_FEW_PAIRS pairs
+    const bool many = tc && R * (c.n_q_heads / c.n_kv_heads) > (size_t)KV4_FEW_PAIRS;
+    const size_t slots = many ? std::max(few, KV4_MANY_SLOTS) : few;
     w.kv4_part = (float*)take(slots * c.head_dim * 4);
     w.kv4_ml = (float2*)take(slots * sizeof(float2));
     w.kv4_counter_bytes = (size_t)(KV4_ROWS * c.n_q_heads / 8 + c.n_kv_heads) * sizeof(int);
@@ -606,7 +610,7 @@ clasp::kv4::View kv4_view(const clasp_ctx* ctx, void* p, int64_t capacity) {
 // kernel of one-token decoding, so that a row's sums do not depend on the rows that share the call.  fp32 models stay there.
 bool kv4_takes_many(const clasp_config& c, const clasp::kv4::AttnArgs& p) {
   if (c.dtype != CLASP_BF16 || (c.flags & CLASP_FLAG_FORCE_SIMT)) return false;
-  return p.own_n > 0 ? p.R_all * (c.n_q_heads / c.n_kv_heads) > 16 : p.R_all > KV4_FEW_ROWS;
+  return p.own_n > 0 ? p.R_all * (c.n_q_heads / c.n_kv_heads) > KV4_FEW_PAIRS : p.R_all > KV4_FEW_ROWS;
 }
 
 template <int HD, bool SPLIT>

@@ -176,21 +176,23 @@ def cmd_trace(args):
 
 def cmd_decode(args):
     max_ctx = args.prompt + args.new + 4 * (max(args.K) + 1) + 64
-    cfg, ccfg, eng, keep = build_engine(args.model, max_ctx, max(args.M), 1, max_head_rows=max(args.K) + 1)
+    cfg, ccfg, eng, keep = build_engine(args.model, max_ctx, max(args.M), 1, max_head_rows=max(args.K) + 1,
+                                        flags=clasp.FLAG_KV4 if args.kv4 else 0)
+    Cache = clasp.KV4Cache if args.kv4 else clasp.KVCache
     prompt = datagen.token_ids(cfg, args.prompt, stream=7).tolist()
     a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-    kv = clasp.KVCache(ccfg, device=eng.device)
+    kv = Cache(ccfg, device=eng.device)
     torch.cuda.synchronize()
     a.record(eng.stream)
     ar = greedy_autoregressive(eng, kv, prompt, args.new)
     b.record(eng.stream)
     torch.cuda.synchronize()
     ar_ms = a.elapsed_time(b)
-    print(json.dumps({"what": "autoregressive", "model": cfg.name, "prompt": args.prompt, "new": args.new,
+    print(json.dumps({"what": "autoregressive", "model": cfg.name, "prompt": args.prompt, "new": args.new, "kv4": args.kv4,
                       "total_ms_incl_prefill": round(ar_ms, 2)}), flush=True)
     for M in args.M:
         for K in args.K:
-            kv = clasp.KVCache(ccfg, device=eng.device)
+            kv = Cache(ccfg, device=eng.device)
             dec = clasp.SelfSpeculativeDecoder(eng, kv, M=M, K=K, dp_interval=args.dp_interval, time_stages=True)
             torch.cuda.synchronize()
             a.record(eng.stream)
@@ -247,6 +249,7 @@ def main():
     p.add_argument("--K", type=int, nargs="+", default=[4])
     p.add_argument("--M", type=int, nargs="+", default=[12])
     p.add_argument("--dp-interval", type=int, default=1)
+    p.add_argument("--kv4", action="store_true", help="key/value cache held in 4 bits")
     args = ap.parse_args()
     {"dp": cmd_dp, "decode": cmd_decode, "trace": cmd_trace}[args.cmd](args)
 

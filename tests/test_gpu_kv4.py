@@ -353,6 +353,35 @@ def test_captured_calls_follow_their_inputs():
             assert (np.abs(ref.to_np(want) - full) <= ref.tolerance(full, spread, vmax, True)).all()
 
 
+@pytest.mark.parametrize("R,own", [(40, False), (24, True)])
+def test_captured_calls_of_many_rows(R, own):
+    """Attention of many rows, its keys cut into parts and joined, captured once and replayed on new inputs."""
+    heads, cap, ctx = (32, 8, 128), 2048, 1500
+    stream = torch.cuda.Stream()
+    n_q, n_kv, hd = heads
+    with torch.cuda.stream(stream):
+        eng, kv = make(heads, cap)
+        q = torch.zeros((R, n_q, hd), dtype=torch.bfloat16, device="cuda")
+        out = torch.empty_like(q)
+        call = lambda o: eng.kv4_attention(q, kv, ctx, own_pos0=ctx if own else None, out=o)
+        call(out)
+        stream.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            eng.kv4_attention(q, kv, ctx, own_pos0=ctx if own else None, out=out)
+        for seed in (1, 2):
+            q.copy_(rows(seed, (R, n_q, hd), "bf16"))
+            eng.kv4_write(rows(seed + 5, (ctx + R, n_kv, hd), "bf16").cuda(), rows(seed + 7, (ctx + R, n_kv, hd), "bf16").cuda(), 0, kv)
+            g.replay()
+            g.replay()
+            want = call(torch.empty_like(q))
+            stream.synchronize()
+            assert torch.equal(out, want)
+            kk, vv = (ref.unpack(b[0].cpu().numpy(), n_kv, cap, hd)[:ctx + (R if own else 0)] for b in (kv.k, kv.v))
+            full, spread, vmax = ref.attention(ref.to_np(q), kk, vv, ref.seen_mask(R, 1, ctx, own))
+            assert (np.abs(ref.to_np(want) - full) <= ref.tolerance(full, spread, vmax, True)).all()
+
+
 def test_positions_past_four_gigabytes():
     """A cache whose byte offsets need more than 32 bits: rows at its end are written, read and attended to."""
     heads, cap = (8, 8, 128), 9_000_000        # 4.6 GB of key codes
@@ -455,6 +484,21 @@ def test_refusals_of_the_binding():
         eng.kv4_attention(q, kv, 4, own_pos0=-1)
     with pytest.raises(ValueError):
         eng.kv4_attention(q, kv, 4, out=q[:1])
+    for call in (lambda: eng.kv4_write(k, k, 1 << 32, kv), lambda: eng.kv4_read(-(1 << 32), 1, kv),
+                 lambda: eng.kv4_attention(q, kv, (1 << 32) + 4), lambda: eng.kv4_attention(q, kv, 4, own_pos0=1 << 33)):
+        with pytest.raises(ValueError):
+            call()
+    # a cache of another kind or layout
+    other = clasp.KV4Cache(make((8, 2, 128), 31)[0].cfg)
+    plain = clasp.ClaspConfig.from_buffer_copy(eng.cfg)
+    plain.flags = 0
+    for bad in (other, clasp.KVCache(plain)):
+        with pytest.raises(ValueError):
+            eng.kv4_write(k, k, 0, bad)
+        with pytest.raises(ValueError):
+            eng.verify(torch.zeros(1, dtype=torch.int32, device="cuda"), 0, bad, 0, want_hidden=False)
+    with pytest.raises(ValueError):
+        clasp.Clasp(plain).verify(torch.zeros(1, dtype=torch.int32, device="cuda"), 0, kv, 0, want_hidden=False)
     with pytest.raises(clasp.ClaspError):
         eng.kv4_read(31, 2, kv)
     with pytest.raises(ValueError):

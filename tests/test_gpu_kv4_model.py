@@ -215,3 +215,34 @@ def test_moving_a_cache_between_the_two_forms(model):
     want, _, _ = layer_with(cfg, b[:, 0].double().cpu().numpy(), model.oracle.layer(0), k[:CTX + 1], v[:CTX + 1], CTX, CTX)
     assert close_hidden(b[:, 1].double().cpu().numpy(), want, tol_hidden(cfg))
     assert rel_l2(a[:, 1].cpu().numpy(), b[:, 1].cpu().numpy()) < 0.1
+
+
+@pytest.mark.parametrize("flag", [clasp.FLAG_PRUNE, clasp.FLAG_FORCE_SIMT])
+def test_with_the_other_flags(model, flag):
+    """The search without its unreachable states, and the CUDA-core products of a bf16 model, on the same kind of cache."""
+    cfg, M = model.cfg, 3
+    eng = model.engine_with_flags(clasp.FLAG_KV4 | flag)
+    kv = clasp.KV4Cache(model.ccfg)
+    toks = datagen.token_ids(cfg, CTX + 1).cuda()
+    model.engine.verify(toks[:CTX], 0, kv, 0, want_hidden=False)
+    _, hid = model.engine.verify(toks[CTX:], CTX, kv, 1)
+    hid = hid[0].contiguous()
+    a = model.engine.dp_search(hid, cfg.d_model, 0, kv, CTX, CTX, 1, M)
+    b = eng.dp_search(hid, cfg.d_model, 0, kv, CTX, CTX, 1, M)
+    D, E = a["D"].cpu().numpy(), b["D"].cpu().numpy()
+    if flag == clasp.FLAG_PRUNE:
+        ok = ~np.isnan(E)
+        assert np.array_equal(D[ok], E[ok]) and torch.equal(a["S"], b["S"]) and torch.equal(a["g_final"], b["g_final"])
+    else:
+        # first cells only: a rounding may move a decision further down
+        np.testing.assert_allclose(D[:3], E[:3], atol=1e-3)
+    n = 70                               # rows of one launch of the few-row attention and more
+    long = datagen.token_ids(cfg, CTX + n).cuda()
+    kv2 = clasp.KV4Cache(model.ccfg)
+    eng.verify(long[:CTX], 0, kv2, 0, want_hidden=False)
+    _, h = eng.verify(long[CTX:], CTX, kv2, 1)
+    h = h.double().cpu().numpy()
+    k, v = held(model, kv2, 0)
+    want, _, _ = layer_with(cfg, h[:, 0], model.oracle.layer(0), k[:CTX + n], v[:CTX + n], CTX, CTX)
+    assert close_hidden(h[:, 1], want, tol_hidden(cfg))
+    assert eng.device_status() == 0
