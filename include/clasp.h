@@ -285,7 +285,7 @@ int clasp_layer_forward(clasp_ctx* ctx, int32_t layer, const float* x_in, int64_
  * cost more to read per token than the weights).  A context made with CLASP_FLAG_KV4 has such a cache: every call above
  * that takes clasp_kv_layer then takes packed arrays, 9/32 of the bytes of a bf16 cache, and new keys and values are
  * quantised before the rows attend to them (so verification and one-token decoding see the same cache).  Its calls run
- * one kernel per step.
+ * one kernel per step, and clasp_engine_active reads 0.
  *
  * Format.  A block is 16 consecutive dims of one position's key or value, sixteen 4-bit codes c and one scale byte b:
  *     value = (c - 8) * s,   s = the half-precision number with the bits b << 7
@@ -318,7 +318,10 @@ int clasp_kv4_read(clasp_ctx* ctx, const clasp_kv_layer* kv_layer, int32_t pos0,
  * itself, whose keys and values lie at positions own_pos0 + s*T + t (written before; own_pos0 == ctx_len with S == 1 is a
  * verification); own_pos0 == -1: none.  A row that sees nothing gives zeros; a NaN block reaches the rows that see it and no
  * others.  Scores must be finite in fp32.  q, out: [S*T, n_q_heads, head_dim]; they must not overlap.
- * A row's result does not depend on the rows that share the call. */
+ * bf16 models: in calls of up to 16 rows without rows of their own, or whose own rows are a verification, a row's result
+ * is the same bits whatever rows share the call (larger calls, and states of more than 16 rows x query heads per kv head, run
+ * on the tensor cores' large tiles, which sum in another order); fp32 models: in every call without separate own rows.  Scale
+ * bytes that clasp_kv4_write does not make (above 0xC6, other than 0xFF) are for clasp_kv4_read alone. */
 int clasp_kv4_attention(clasp_ctx* ctx, const void* q, int64_t q_stride, int32_t S, int32_t T, int32_t ctx_len,
                         int32_t own_pos0, const int32_t* visible, const clasp_kv_layer* kv_layer, void* out,
                         int64_t out_stride);

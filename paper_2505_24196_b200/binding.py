@@ -19,6 +19,7 @@ CLASP_FP32, CLASP_BF16 = 0, 1
 CHOICE_APPLY, CHOICE_SKIP, CHOICE_NONE = 0, 1, 255
 FLAG_FORCE_SIMT, FLAG_NO_DEFER, FLAG_MULTI_KERNEL, FLAG_PRUNE, FLAG_NO_ATT_TC = 1, 2, 4, 8, 16
 FLAG_KV4 = 32
+MAX_POSITION = 1 << 30     # of a 4-bit cache; the library's numbers have 32 bits, larger ones would come round
 
 SYMBOLS = ["clasp_workspace_bytes", "clasp_create", "clasp_destroy", "clasp_load_layers", "clasp_load_head",
            "clasp_dp_search", "clasp_verify", "clasp_draft_forward", "clasp_accept", "clasp_layer_forward",
@@ -354,11 +355,6 @@ class Clasp:
             raise ValueError(f"no layer {layer}")
         return kv.layers[layer]
 
-    def _positions(self, *at: int):
-        for v in at:                    # (the library's numbers have 32 bits: larger ones would come round)
-            if not -1 <= v <= 1 << 30:
-                raise ValueError(f"{v}: not a position or a number of rows")
-
     def kv4_write(self, k: torch.Tensor, v: torch.Tensor, pos0: int, kv: KV4Cache, layer: int = 0):
         """Quantise rows k, v [n, n_kv_heads, head_dim] into positions pos0.. of one layer of a 4-bit cache."""
         h = self._nkv
@@ -366,7 +362,8 @@ class Clasp:
         n = k.shape[0]
         if v.shape[0] != n:
             raise ValueError("k and v: as many rows")
-        self._positions(pos0)
+        if not 0 <= pos0 <= MAX_POSITION:
+            raise ValueError("pos0: a position")
         _check(self.lib.clasp_kv4_write(self.handle, k.data_ptr(), ks, v.data_ptr(), vs, n, pos0, self._kv4_layer(kv, layer)),
                "clasp_kv4_write")
 
@@ -374,9 +371,10 @@ class Clasp:
                  v_out: Optional[torch.Tensor] = None):
         """Rows pos0..pos0+n-1 of one layer of a 4-bit cache in the model dtype: (k, v), each [n, n_kv_heads, head_dim]."""
         h = self._nkv
-        if n < 0:
-            raise ValueError("n: a number of rows")
-        self._positions(pos0, n)
+        if not 0 <= n <= MAX_POSITION or not 0 <= pos0 <= MAX_POSITION:
+            raise ValueError("pos0, n: a position and a number of rows")
+        if pos0 + n > self._layout[1]:
+            raise ClaspError(-3, "clasp_kv4_read")      # (before memory for the rows is asked for)
         if k_out is None and v_out is None:
             shape = (n, h, self._hd)
             k_out, v_out = self._new_rows(self._like.new_empty(shape)), self._new_rows(self._like.new_empty(shape))
@@ -407,9 +405,10 @@ class Clasp:
             raise ValueError(f"visible: int32 [{R}] on {q.device} expected")
         if own_pos0 is None:
             own_pos0 = -1
-        elif own_pos0 < 0:
+        elif not 0 <= own_pos0 <= MAX_POSITION:
             raise ValueError("own_pos0: a position")
-        self._positions(ctx_len, own_pos0)
+        if not 0 <= ctx_len <= MAX_POSITION:
+            raise ValueError("ctx_len: a number of positions")
         if out is None:
             out, os = self._new_rows(torch.empty_like(q)), h * self._hd    # (rows with gaps give rows without)
         else:
