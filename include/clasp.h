@@ -293,7 +293,7 @@ int clasp_layer_forward(clasp_ctx* ctx, int32_t layer, const float* x_in, int64_
  * saturate), c - 8 = x / s to the nearest, ties to even.  A block that holds an infinity or NaN gets b = 0xFF and reads
  * back as NaN throughout.  The bytes are a function of the row alone; every value is exact in bf16.  The array of one
  * layer's keys (or values): codes [n_kv_heads, max_ctx, head_dim / 2], low nibble first, then scale bytes
- * [n_kv_heads, max_ctx, head_dim / 16]; 16-byte aligned.  max_ctx is at most 2^30.
+ * [n_kv_heads, max_ctx, head_dim / 16]; 16-byte aligned.  max_ctx is at most 2^30, n_kv_heads 2^14.
  *
  * The calls below need a context made with CLASP_FLAG_KV4 and its device current, run on its stream and use its
  * workspace (calls, and captured graphs of calls, on one context must not overlap on the GPU).  Rows of heads are in the

@@ -187,7 +187,7 @@ class KV4Cache:
             self.array[l].k = self.k[l].data_ptr()
             self.array[l].v = self.v[l].data_ptr()
         self.layers = [C.pointer(self.array[l]) for l in range(cfg.L)]
-        self.layout = (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim)
+        self.layout = (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim, self.k.get_device())
 
 
 class Clasp:
@@ -207,7 +207,8 @@ class Clasp:
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         # what the calls on single tokens read each time
         self._index, self._stream_ptr = self.workspace.get_device(), self.stream.cuda_stream
-        self._kv4, self._layout = bool(cfg.flags & FLAG_KV4), (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim)
+        self._kv4 = bool(cfg.flags & FLAG_KV4)
+        self._layout = (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim, self._index)
         self._hd, self._nq, self._nkv = cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
         self._like = torch.empty(0, dtype=self.dtype, device=self.workspace.device)
         handle = C.c_void_p()
@@ -250,7 +251,7 @@ class Clasp:
         if isinstance(kv, KV4Cache) != self._kv4:
             raise ValueError("contexts made with FLAG_KV4 take a KV4Cache, others a KVCache")
         if self._kv4 and kv.layout != self._layout:
-            raise ValueError(f"cache of (layers, positions, kv heads, head_dim) {kv.layout}, context of {self._layout}")
+            raise ValueError(f"cache of (layers, positions, kv heads, head_dim, device) {kv.layout}, context of {self._layout}")
         return kv.array
 
     # ---- the calls of the hot path
