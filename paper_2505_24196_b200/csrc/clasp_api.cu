@@ -622,21 +622,12 @@ int kv4_rows_launch(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
   return launch_check(ctx);
 }
 
-template <int HD, int NB>
-int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
+// Joins the parts.  Its launch overlaps the attention's end (the kernel itself waits for it): 0.8 us.
+template <int HD, int NB, int BATCH>
+int kv4_merge(clasp_ctx* ctx, const clasp::kv4::AttnArgs& p) {
   namespace k4 = clasp::kv4;
-  const int pairs = p.R * (p.nq / p.nkv);
-  p.blocks = (pairs + NB * k4::TP - 1) / (NB * k4::TP);
-  // few blocks: their key tiles are split so that every SM has work
-  const int items = p.blocks * p.nkv, keys = p.n_keys + (p.own_n > 0 ? std::min(p.own_n, NB * k4::TP + p.T) : 0);
-  p.splits = std::max(1, std::min(ctx->num_sms / items, (keys + k4::TK - 1) / k4::TK));
-  p.splits = std::min(p.splits, std::max(1, (int)(KV4_MANY_SLOTS / ((size_t)items * NB * k4::TP))));
-  k4::attn_many_kernel<HD, NB><<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
-  int rc = launch_check(ctx);
-  if (rc || p.splits == 1) return rc;
-  // its launch overlaps the attention's end (the kernel itself waits for it): 12 states over 8192 positions 18.3 -> 17.5 us
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3(items * (HD / 4) * NB / 2);
+  lc.gridDim = dim3(p.blocks * p.nkv * (NB * k4::TP / 8) * (HD / k4::merge_dims<HD, BATCH>));
   lc.blockDim = dim3(256);
   lc.stream = ctx->stream;
   cudaLaunchAttribute attr{};
@@ -644,8 +635,24 @@ int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   lc.attrs = &attr;
   lc.numAttrs = 1;
-  CUDA_TRY(cudaLaunchKernelEx(&lc, k4::merge_kernel<HD, NB>, p));
+  CUDA_TRY(cudaLaunchKernelEx(&lc, k4::merge_kernel<HD, NB, BATCH>, p));
   return launch_check(ctx);
+}
+
+template <int HD, int NB>
+int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
+  namespace k4 = clasp::kv4;
+  const int pairs = p.R * (p.nq / p.nkv);
+  p.blocks = (pairs + NB * k4::TP - 1) / (NB * k4::TP);
+  // few blocks: their key tiles are split so that every SM has work
+  const int items = p.blocks * p.nkv, keys = p.n_keys + (p.own_n > 0 ? std::min(p.own_n, NB * k4::TP + p.T) : 0);
+  p.splits = std::max(1, std::min({ctx->num_sms / items, (keys + k4::TK - 1) / k4::TK, k4::MAX_SPLITS}));
+  p.splits = std::min(p.splits, std::max(1, (int)(KV4_MANY_SLOTS / ((size_t)items * NB * k4::TP))));
+  k4::attn_many_kernel<HD, NB><<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
+  int rc = launch_check(ctx);
+  if (rc || p.splits == 1) return rc;
+  if (p.splits <= 3) return kv4_merge<HD, NB, 3>(ctx, p);
+  return p.splits <= 9 ? kv4_merge<HD, NB, 9>(ctx, p) : kv4_merge<HD, NB, 18>(ctx, p);
 }
 
 // Attention of `p.R_all` rows described by p (q, out, views, masks) over the cache and the own rows.
@@ -667,7 +674,11 @@ int kv4_attend(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
     p.status = ctx->ws.status;
     p.spin_fast = ctx->wait_limit ? std::min(ctx->wait_limit, clasp::tc::SPIN_FAST) : clasp::tc::SPIN_FAST;
     p.spin_slow = ctx->wait_limit ? ctx->wait_limit : clasp::tc::SPIN_SLOW;
-    const bool one = p.R * (p.nq / p.nkv) <= clasp::kv4::TP;
+    // One block of pairs per CTA where that gives every block an SM of its own and there is nothing to gain from sharing tiles: the
+    // blocks need no parts, or the keys are few (400 rows of 32 heads 13.9 us, two blocks per CTA in two parts 20; 200 rows over
+    // 4000 positions 36 with one, 33 with two)
+    const long long pairs = (long long)p.R * (p.nq / p.nkv), blocks = (pairs + clasp::kv4::TP - 1) / clasp::kv4::TP * p.nkv;
+    const bool one = pairs <= clasp::kv4::TP || (blocks <= ctx->num_sms && (2 * blocks > ctx->num_sms || p.n_keys < 2048));
     if (c.head_dim == 128) return one ? kv4_many_launch<128, 1>(ctx, p) : kv4_many_launch<128, 2>(ctx, p);
     return one ? kv4_many_launch<64, 1>(ctx, p) : kv4_many_launch<64, 2>(ctx, p);
   }

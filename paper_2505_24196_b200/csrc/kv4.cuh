@@ -892,8 +892,8 @@ static_assert(sizeof(ManyShared) <= 2048, "fits its share of shared memory");
 // tile's Q K^T runs under this tile's softmax.  NaN blocks: as in attn_rows_kernel; where a value's NaN block was met, the pairs
 // look through the scale bytes of the keys they see once more at the end.
 //
-// Measured, 32 query heads over eight kv heads of 128, us: a prompt of 1999 rows 49, 128 rows over 4095 positions 26.2 with its
-// merge, twelve states over 8192 17.5.  A tile of 2 x 128 pairs takes 2000 cycles where its multiplies take 1280 and its
+// Measured, 32 query heads over eight kv heads of 128, us: a prompt of 1999 rows 49, 128 rows over 4095 positions 22.8 with its
+// merge, twelve states over 8192 19.4.  A tile of 2 x 128 pairs takes 2000 cycles where its multiplies take 1280 and its
 // exponentials 1024: bound by the softmax warps' chain (scores from tensor memory, maximum, exponentials, weights back, barrier),
 // two warps per scheduler in step.  No gain from a quarter of the exponentials on the multiply-add pipe, from exponentials with
 // the previous maximum while the new one is found, nor from starting the blocks half a tile apart (51.8, 55.3, 56.8 us against
@@ -1323,52 +1323,78 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
   }
 }
 
-// The parts of each pair of attn_many_kernel, in their order.  A thread takes four dims of a pair; neighbouring threads
-// neighbouring pairs, as the parts lie.  Sixteen parts' loads are in flight at a time.
-template <int HD, int NB>
+// The parts of each pair of attn_many_kernel, in their order: eight pairs per CTA (whole sectors of the parts, where pairs lie side
+// by side), a thread takes HD / 32 dims of one -- two where the parts are many and the pairs few --, and the rows go out through
+// shared memory.  (A thread per four dims of a pair, pairs
+// on neighbouring lanes, left an eighth of a sector per store: 28 us where 400 rows of 32 heads were cut in two.)  All parts are fetched
+// at once up to BATCH of them: 3, 9 or 18, since what is not there costs its instructions too (400 rows in two parts 18 / 20 / 27 us
+// with the attention, twelve states in 18 parts 24.7 / 21.5 / 19.2).
+constexpr int MAX_SPLITS = 148;
+template <int HD, int BATCH> constexpr int merge_dims = BATCH > 9 ? 64 : HD;
+template <int HD, int NB, int BATCH>
 __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ AttnArgs p) {
-  constexpr int PAIRS = NB * TP, CHUNKS = 256 / PAIRS, PER = HD / 4 / CHUNKS;   // pieces of four dims per CTA, CTAs per item
-  const int item = blockIdx.x / PER, chunk = blockIdx.x % PER * CHUNKS + (int)threadIdx.x / PAIRS;
-  const int pair = threadIdx.x % PAIRS, Gq = p.nq / p.nkv;
-  const int kvh = item % p.nkv, pp = (p.blocks - 1 - item / p.nkv) * PAIRS + pair;
+  constexpr int PAIRS = NB * TP, GROUP = 8, DIMS = merge_dims<HD, BATCH>, E = DIMS / 32, PER = PAIRS / GROUP * (HD / DIMS);
+  __shared__ float w_sm[MAX_SPLITS][GROUP], den_sm[GROUP];
+  __shared__ __align__(16) float o_sm[GROUP][DIMS + 4];
+  const int item = blockIdx.x / PER, first = blockIdx.x % PER / (HD / DIMS) * GROUP, dim0 = blockIdx.x % (HD / DIMS) * DIMS;
+  const int Gq = p.nq / p.nkv;
+  const int kvh = item % p.nkv, pair0 = (p.blocks - 1 - item / p.nkv) * PAIRS + first;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // (launched while the parts are still being made)
-  if (pp >= p.R * Gq) return;
-  const float2* ml = p.part_ml + (long long)item * p.splits * PAIRS + pair;
-  const float* src = p.part + ((long long)item * p.splits * HD + chunk * 4) * PAIRS + pair;
-  float mx = -INFINITY, den = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-  for (int i0 = 0; i0 < p.splits; i0 += 16) {
-    float2 v[16];
-    float x[16][4];
+  if (pair0 >= p.R * Gq) return;
+  const int pair = threadIdx.x % GROUP, d0 = threadIdx.x / GROUP;
+  const float* src = p.part + ((long long)item * p.splits * HD + dim0 + d0) * PAIRS + first + pair;
+  float x[BATCH][E];                       // the parts on their way, BATCH at a time
+  auto load = [&](int i0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[i] = make_float2(-INFINITY, 0.f);
-      if (i0 + i < p.splits) v[i] = __ldcg(ml + (i0 + i) * PAIRS);
+    for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[b][e] = i0 + b < p.splits ? __ldcg(src + ((long long)(i0 + b) * HD + e * 32) * PAIRS) : 0.f;
+  };
+  load(0);
+  {                                        // the parts' weights: a warp per pair, a lane per part
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float2* ml = p.part_ml + (long long)item * p.splits * PAIRS + first + w;
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll 1
+    for (int i = lane; i < p.splits; i += 32) mx = fmaxf(mx, __ldcg(ml + i * PAIRS).x);
+#pragma unroll
+    for (int e = 16; e > 0; e >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, e));
+#pragma unroll 1
+    for (int i = lane; i < p.splits; i += 32) {
+      const float2 v = __ldcg(ml + i * PAIRS);
+      const float f = v.x == -INFINITY ? (v.y == v.y ? 0.f : 1.f) : exp2f(v.x - mx);   // (a sum without a maximum is 0, or NaN)
+      w_sm[i][w] = f;
+      sum = fmaf(v.y, f, sum);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int e = 16; e > 0; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
+    if (lane == 0) den_sm[w] = sum;
+  }
+  __syncthreads();
+  const float den = den_sm[pair];
+  float a[E];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] = i0 + i < p.splits ? __ldcg(src + ((long long)(i0 + i) * HD + e) * PAIRS) : 0.f;
-    float m2 = mx;
+  for (int e = 0; e < E; ++e) a[e] = 0.f;
+#pragma unroll 1
+  for (int i0 = 0; i0 < p.splits; i0 += BATCH) {
+    if (i0 > 0) load(i0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m2 = fmaxf(m2, v[i].x);
-    const float corr = mx == -INFINITY ? 1.f : exp2f(mx - m2);      // (nothing so far, or sums without a maximum: NaN)
-    den *= corr;
+    for (int b = 0; b < BATCH; ++b) {
+      const float f = i0 + b < p.splits ? w_sm[i0 + b][pair] : 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) a[e] *= corr;
-    mx = m2;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float w = v[i].x == -INFINITY ? (v[i].y == v[i].y ? 0.f : 1.f) : exp2f(v[i].x - mx);
-      den = fmaf(v[i].y, w, den);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) a[e] = fmaf(w, x[i][e], a[e]);
+      for (int e = 0; e < E; ++e) a[e] = fmaf(f, x[b][e], a[e]);
     }
   }
   const float inv = den == 0.f ? 0.f : 1.0f / den;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o_sm[pair][d0 + e * 32] = a[e] * inv;
+  __syncthreads();
+  const int row = threadIdx.x / (DIMS / 8), c = threadIdx.x % (DIMS / 8) * 8, pp = pair0 + row;
+  if (row >= GROUP || pp >= p.R * Gq) return;
+  const float4 u = *reinterpret_cast<const float4*>(&o_sm[row][c]), v = *reinterpret_cast<const float4*>(&o_sm[row][c + 4]);
   const int r = pp / Gq;
-  *reinterpret_cast<uint2*>((bf16*)p.out + (long long)r * p.out_stride + (long long)(kvh * Gq + pp - r * Gq) * HD + chunk * 4) =
-      make_uint2(pack_bf16(a[0] * inv, a[1] * inv), pack_bf16(a[2] * inv, a[3] * inv));
+  *reinterpret_cast<uint4*>((bf16*)p.out + (long long)r * p.out_stride + (long long)(kvh * Gq + pp - r * Gq) * HD + dim0 + c) =
+      make_uint4(pack_bf16(u.x, u.y), pack_bf16(u.z, u.w), pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
 }  // namespace kv4
