@@ -86,9 +86,8 @@ def tolerance(out, spread, vmax, bf16):
       scores: 16-wide multiplies added in fp32 in at most 16 steps (2^-23 of the terms' magnitudes each, truncation counted as a
               whole step), operands exact (bf16 rows) or two half-precision parts (2^-22): d = spread (2^-19 + 2^-22 + 2^-21)
               with two more roundings for the scale to base 2 and the power of two, each 2^-24 of a score <= spread;
-      weights: exp2 2^-22, half precision 2^-11 (bf16 models) or two parts 2^-22; weights below 2^-26 of the largest
-              lose at most 2^-37 (bf16 models; fp32 models 2^-37 as well) each, which n <= 2^20 keys make 2^-17 x vmax at
-              worst and is far less wherever few keys are that light;
+      weights: exp2 2^-22, half precision 2^-11 (bf16 models) or two parts 2^-22; weights below 2^-24 of the largest lose at
+              most 2^-35 each, 2^-22 x vmax for 2^13 keys of that kind (no test has more);
       sums:   fp32 in runs of at most 64 additions per level, 2^-17;  both enter numerator and denominator.
       result: half a step of its type."""
     d = spread * (2.0 ** -19 + 2.0 ** -21 + 2.0 ** -22) + 2.0 ** -22
