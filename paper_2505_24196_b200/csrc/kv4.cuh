@@ -6,8 +6,8 @@
 // nearest, ties to even.  Every step of that is exact in fp32 (7 s has 7 significant bits, a border (k + 1/2) s has 8, a
 // correctly rounded quotient never reaches a border that x / s does not), so the bytes are a function of the row alone.  A
 // value has at most 8 significant bits: exact in bf16 and in half precision.  Sixteen dims per scale: uniform steps of
-// 2/15 of a block's range leave a Gaussian row 7.7 % of its standard deviation as error (4-bit floating point with the same
-// scale byte 9.6 %).  A block that holds an infinity or NaN gets the byte 0xFF and reads back as NaN throughout.
+// a seventh of a block's largest magnitude leave a Gaussian row 9.3 % of its standard deviation as error (4-bit floating point
+// with the same scale byte 10.0 %).  A block that holds an infinity or NaN gets the byte 0xFF and reads back as NaN throughout.
 //
 // One layer's array (keys or values): codes [n_kv, capacity, hd / 2], low nibble first, then scale bytes
 // [n_kv, capacity, hd / 16].  Head-major: what one CTA of the attention reads is contiguous.
