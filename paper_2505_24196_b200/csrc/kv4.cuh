@@ -778,8 +778,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
   auto store = [&](const float4& a, float den) {
     const float inv = den == 0.f ? 0.f : 1.0f / den;
     const long long at = (long long)r * p.out_stride + (long long)hq * HD + d;
-    if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + at) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
-    else *reinterpret_cast<float4*>((float*)p.out + at) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    // (+ 0: a zero's sign would tell whether the call had runs that the pair sees nothing of)
+    const float4 y = make_float4(fmaf(a.x, inv, 0.f), fmaf(a.y, inv, 0.f), fmaf(a.z, inv, 0.f), fmaf(a.w, inv, 0.f));
+    if constexpr (!SPLIT) *reinterpret_cast<uint2*>((bf16*)p.out + at) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    else *reinterpret_cast<float4*>((float*)p.out + at) = y;
   };
   if (group == 0 && on) {
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -837,13 +839,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(const __grid_c
     if (lane == 0) den_sm[warp] = den;
   }
   __syncthreads();
-  // groups of threads share the runs between them
-  const int per = (parts + GROUPS - 1) / GROUPS, last_run = min(parts, (group + 1) * per);
+  // groups of threads share the runs between them: run i is group i % GROUPS', however many runs the call has (others' rows may
+  // reach into runs that this pair sees nothing of), so that a row's sum does not depend on the rows that share the call
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   if (on) {
     const float* src = p.part + rh * parts * HD + d;
 #pragma unroll 9
-    for (int i = group * per; i < last_run; ++i) {
+    for (int i = group; i < parts; i += GROUPS) {
       const float4 v = __ldcg(reinterpret_cast<const float4*>(src + (long long)i * HD));
       const float w = wr_sm[col * MAX_PARTS + i];
       a.x = fmaf(w, v.x, a.x); a.y = fmaf(w, v.y, a.y); a.z = fmaf(w, v.z, a.z); a.w = fmaf(w, v.w, a.w);
