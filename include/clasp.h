@@ -90,7 +90,9 @@ typedef struct clasp_config {
 #define CLASP_FLAG_PRUNE 8      /* the search leaves out the states from which (L, M) can no longer be
                                    reached, j < M - (L - i): Algorithm 1 computes them, but the backtrack
                                    can never visit them.  Skip mask, g[L][M] and every reachable cell are
-                                   unchanged; the cells left out read NaN in `scores` and `margins`. */
+                                   unchanged; the cells left out read NaN in `scores` and `margins`.
+                                   (With CLASP_FLAG_KV4 the states are carried all the same, since a
+                                   step's kernel depends on how many there are: the flag saves no work.) */
 #define CLASP_FLAG_MULTI_KERNEL 4 /* diagnostics: one kernel per step (GEMM, attention, norm,
                                    Eq. 2 select ...) instead of the persistent kernel (bf16) or
                                    the one-cluster kernel (small fp32 models) that runs a whole

@@ -1683,7 +1683,11 @@ int clasp_dp_search(clasp_ctx* ctx, const float* hidden_states, int64_t layer_st
   int cur = 0;
   for (int i = 1; i <= L; ++i) {
     const int ell = (i - 1 < M) ? i - 1 : M;
-    const int j_lo = (prune && M - (L - i) > 1) ? M - (L - i) : 1;   // first state the step carries
+    const int j_show = (prune && M - (L - i) > 1) ? M - (L - i) : 1;   // first state whose cell is reported
+    // First state the step carries.  Over a 4-bit cache the kernel, the parts its keys are cut into and the place of a state's own
+    // rows depend on the states that share the step, so there all are carried: the cells that count stay the same bits.  (The last M
+    // of L steps take all M states instead of M / 2 on average; their weights are read once either way.)
+    const int j_lo = is_kv4(c) ? 1 : j_show;
     const int n = ell - j_lo + 1 > 0 ? ell - j_lo + 1 : 0;
     float* g_prev = ws.grow[cur];
     float* g_next = ws.grow[cur ^ 1];
@@ -1702,7 +1706,7 @@ int clasp_dp_search(clasp_ctx* ctx, const float* hidden_states, int64_t layer_st
     a.margin = margins ? margins + (int64_t)i * (M + 1) : nullptr;
     a.choice = ws.choice + (int64_t)i * (M + 1);
     a.forced = forced_choice ? forced_choice + (int64_t)i * (M + 1) : nullptr;
-    a.T = T; a.d = d; a.ell = n; a.i = i; a.M = M; a.j_lo = j_lo;
+    a.T = T; a.d = d; a.ell = n; a.i = i; a.M = M; a.j_lo = j_lo; a.j_show = j_show;
     const int blocks = 1 + n + (i <= M ? 1 : 0);
     clasp::dp_step_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
     if ((rc = launch_check(ctx))) return rc;

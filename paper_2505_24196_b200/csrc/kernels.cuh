@@ -405,6 +405,7 @@ struct DpStepArgs {
   const uint8_t* forced;  // row i or null
   int T, d, ell, i, M;
   int j_lo;               // first state the step carries (1, or later when unreachable states are left out)
+  int j_show;             // first state whose cell is reported; those before it read NaN
 };
 
 __device__ __forceinline__ void block_sum3(double (&v)[3], double* sh) {
@@ -481,8 +482,9 @@ __global__ void dp_step_kernel(DpStepArgs a) {
     int take = s_app > s_skip;
     if (a.forced && a.forced[j] != 255) take = (a.forced[j] == 0);
     s_take_apply = take;
-    a.D[j] = take ? s_app : s_skip;
-    if (a.margin) a.margin[j] = s_app - s_skip;
+    const bool show = j >= a.j_show;
+    a.D[j] = show ? (take ? s_app : s_skip) : __int_as_float(0x7fc00000);
+    if (a.margin) a.margin[j] = show ? s_app - s_skip : __int_as_float(0x7fc00000);
     a.choice[j] = take ? 0 : 1;
   }
   __syncthreads();
