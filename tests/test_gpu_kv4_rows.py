@@ -1,10 +1,11 @@
-"""Rows read from a 4-bit cache: every byte in both types."""
+"""Rows written to and read from a 4-bit cache: every byte in both types, addresses and strides that are multiples of 16 bytes
+and of no more."""
 import numpy as np
 import pytest
 import torch
 
 import kv4_ref as ref
-from test_gpu_kv4 import make
+from test_gpu_kv4 import dt, make, special_rows
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +29,39 @@ def test_read_every_code_and_scale_in_both_types(dtype, hd):
         want = ((np.arange(16) - 8.0) * half[b][..., None]).reshape(n_kv, cap, hd).transpose(1, 0, 2)
     for got in eng.kv4_read(0, cap, kv):
         np.testing.assert_array_equal(ref.to_np(got), want)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 2, 64), (8, 1, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("offset,pad", [(16, 0), (0, 16), (16, 16), (32, 0), (0, 32), (48, 80)])
+def test_rows_at_multiples_of_sixteen_bytes(heads, dtype, offset, pad):
+    """Rows `offset` bytes behind a 32-byte border and `pad` bytes apart: written, read back and left alone around them."""
+    n_q, n_kv, hd = heads
+    esz = 2 if dtype == "bf16" else 4
+    n, row, cap = 37, n_kv * hd, 64
+    stride, start = row + pad // esz, offset // esz
+    eng, kv = make(heads, cap, dtype=dtype)
+
+    def place(fill):
+        buf = torch.full((start + n * stride + 64,), fill, dtype=dt(dtype), device="cuda")
+        assert buf.data_ptr() % 32 == 0
+        return buf, buf[start:start + n * stride].view(n, stride)[:, :row].unflatten(1, (n_kv, hd))
+
+    x = [special_rows(n, n_kv, hd, dtype, s) for s in (11, 23)]
+    src = [place(5.0)[1] for _ in x]
+    for s, t in zip(src, x):
+        s.copy_(t)
+    kv.k.fill_(0xA5)
+    kv.v.fill_(0xA5)
+    eng.kv4_write(src[0], src[1], 3, kv)
+    dst = [place(9.0) for _ in x]
+    eng.kv4_read(3, n, kv, k_out=dst[0][1], v_out=dst[1][1])
+    torch.cuda.synchronize()
+    for buf, t, (whole, got) in zip((kv.k, kv.v), x, dst):
+        want = np.full(buf.shape[1], 0xA5, dtype=np.uint8)
+        c, b = ref.quantise(ref.to_np(t))
+        ref.pack(c, b, want, n_kv, cap, hd, 3)
+        np.testing.assert_array_equal(buf[0].cpu().numpy(), want)
+        np.testing.assert_array_equal(ref.to_np(got), ref.values(c, b))
+        got.fill_(9.0)
+        assert bool((whole == 9.0).all())
