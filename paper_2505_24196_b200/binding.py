@@ -341,7 +341,7 @@ class Clasp:
         sr, sh, sd = t.stride()
         if (sd != 1 or (sh != hd and heads > 1)) and shape[0]:
             raise ValueError(f"{what}: the heads of a row must be contiguous")
-        return sr if shape[0] > 1 else max(sr, heads * hd)
+        return sr if shape[0] > 1 else heads * hd      # (nothing steps over a single row's stride)
 
     def _new_rows(self, t: torch.Tensor) -> torch.Tensor:
         # memory handed out for another stream than the one that fills it

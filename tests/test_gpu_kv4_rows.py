@@ -1,11 +1,12 @@
 """Rows written to and read from a 4-bit cache: every byte in both types, addresses and strides that are multiples of 16 bytes
-and of no more."""
+and of no more, single rows with any stride."""
 import numpy as np
 import pytest
 import torch
 
 import kv4_ref as ref
-from test_gpu_kv4 import dt, make, special_rows
+import paper_2505_24196_b200 as clasp
+from test_gpu_kv4 import dt, make, rows, special_rows
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,31 @@ def test_rows_at_multiples_of_sixteen_bytes(heads, dtype, offset, pad):
         np.testing.assert_array_equal(ref.to_np(got), ref.values(c, b))
         got.fill_(9.0)
         assert bool((whole == 9.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("odd", [1, 3, 7])
+def test_a_single_row_has_no_stride(dtype, odd):
+    """One row cut from a buffer whose rows are any number of elements apart: nothing steps over that stride."""
+    heads = (8, 2, 128)
+    eng, kv = make(heads, 32, dtype=dtype)
+
+    def one(h):
+        t = torch.zeros((2, h * 128 + odd), dtype=dt(dtype), device="cuda")[:, :h * 128].unflatten(1, (h, 128))[:1]
+        assert t.stride(0) == h * 128 + odd
+        return t
+
+    k, v, q = one(2), one(2), one(8)
+    for i, t in enumerate((k, v, q)):
+        t.copy_(rows(i, tuple(t.shape), dtype))
+    eng.kv4_write(k, v, 4, kv)
+    back = one(2), one(2)
+    eng.kv4_read(4, 1, kv, k_out=back[0], v_out=back[1])
+    out = one(8)
+    assert eng.kv4_attention(q, kv, 4, own_pos0=4, out=out) is out
+    clean = [t.contiguous() for t in (k, v, q)]
+    want = clasp.KV4Cache(eng.cfg)
+    eng.kv4_write(clean[0], clean[1], 4, want)
+    assert torch.equal(kv.k, want.k) and torch.equal(kv.v, want.v)
+    assert all(torch.equal(a, b) for a, b in zip(back, eng.kv4_read(4, 1, kv)))
+    assert torch.equal(out, eng.kv4_attention(clean[2], kv, 4, own_pos0=4))
