@@ -157,6 +157,14 @@ def make_config(model_cfg, max_ctx: int, max_rows: int, max_M: int, max_T: int =
                        max_rows=max_rows, max_M=max_M, max_T=max_T, max_head_rows=max_head_rows, flags=flags)
 
 
+def _settle(t: torch.Tensor):
+    """Waits for the fill of a new cache, so that it may be used on any stream at once."""
+    if t.is_cuda:
+        with torch.cuda.device(t.device):
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()
+
+
 class KVCache:
     """Device KV cache: per layer K and V of shape [max_ctx, n_kv_heads, head_dim]."""
 
@@ -169,6 +177,7 @@ class KVCache:
         for l in range(cfg.L):
             self.array[l].k = self.k[l].data_ptr()
             self.array[l].v = self.v[l].data_ptr()
+        _settle(self.v)
 
 
 class KV4Cache:
@@ -188,6 +197,7 @@ class KV4Cache:
             self.array[l].v = self.v[l].data_ptr()
         self.layers = [C.pointer(self.array[l]) for l in range(cfg.L)]
         self.layout = (cfg.L, cfg.max_ctx, cfg.n_kv_heads, cfg.head_dim, self.k.get_device())
+        _settle(self.v)
 
 
 class Clasp:
@@ -204,7 +214,8 @@ class Clasp:
         nbytes = self.lib.clasp_workspace_bytes(C.byref(cfg))
         if nbytes == 0:
             raise ClaspError(-2, "clasp_workspace_bytes")
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         # what the calls on single tokens read each time
         self._index, self._stream_ptr = self.workspace.get_device(), self.stream.cuda_stream
         self._kv4 = bool(cfg.flags & FLAG_KV4)
@@ -245,6 +256,16 @@ class Clasp:
         _check(self.lib.clasp_load_head(self.handle, head["embed"].data_ptr(), head["final_norm"].data_ptr(),
                                         head["lm_head"].data_ptr()), "clasp_load_head")
 
+    def _empty(self, shape, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+        """Memory for a result (model dtype if none is given).  It comes from the pool of the context's stream, in whose order it is
+        written: a block of the current stream's pool may still be in use by what that stream has queued."""
+        if torch._C._cuda_getCurrentRawStream(self._index) == self._stream_ptr:
+            return self._like.new_empty(shape) if dtype is None else self._like.new_empty(shape, dtype=dtype)
+        with torch.cuda.stream(self.stream):
+            t = self._like.new_empty(shape, dtype=dtype)
+        t.record_stream(torch.cuda.current_stream(self._index))
+        return t
+
     def _array(self, kv):
         """The layers of a cache of the kind and layout this context was made for: a packed cache in place of a plain one, or one
         of another capacity, would be read and written past its end."""
@@ -261,11 +282,10 @@ class Clasp:
         """hidden_states: float32 device tensor; element (l, t, c) at l*layer_stride + t*token_stride + c
         (strides in elements from hidden_states' first element).  Returns a dict of device tensors."""
         L, d = self.cfg.L, self.cfg.d_model
-        dev = self.device
-        mask = torch.empty(L, dtype=torch.uint8, device=dev)
-        scores = torch.empty((L + 1, M + 1), dtype=torch.float32, device=dev)
-        margins = torch.empty((L + 1, M + 1), dtype=torch.float32, device=dev) if want_margins else None
-        g = torch.empty((T, d), dtype=torch.float32, device=dev) if want_g else None
+        mask = self._empty(L, torch.uint8)
+        scores = self._empty((L + 1, M + 1), torch.float32)
+        margins = self._empty((L + 1, M + 1), torch.float32) if want_margins else None
+        g = self._empty((T, d), torch.float32) if want_g else None
         _check(self.lib.clasp_dp_search(self.handle, hidden_states.data_ptr(), layer_stride, token_stride,
                                         self._array(kv), ctx_len, pos0, T, M, mask.data_ptr(), scores.data_ptr(),
                                         _ptr(margins), _ptr(g), _ptr(forced_choice)), "clasp_dp_search")
@@ -277,9 +297,9 @@ class Clasp:
         n = tokens.numel()
         L, d = self.cfg.L, self.cfg.d_model
         if argmax_out is None:
-            argmax_out = torch.empty(max(n_head_rows, 1), dtype=torch.int32, device=self.device)
+            argmax_out = self._empty(max(n_head_rows, 1), torch.int32)
         if want_hidden and hidden_out is None:
-            hidden_out = torch.empty((n, L + 1, d), dtype=torch.float32, device=self.device)
+            hidden_out = self._empty((n, L + 1, d), torch.float32)
         _check(self.lib.clasp_verify(self.handle, tokens.data_ptr(), n, pos0, self._array(kv), n_head_rows,
                                      argmax_out.data_ptr(), _ptr(hidden_out) if want_hidden else None),
                "clasp_verify")
@@ -316,7 +336,7 @@ class Clasp:
     def layer_forward(self, layer: int, x_in: torch.Tensor, S: int, T: int, ctx_len: int, pos0: int,
                       kv: KVCache, write_kv: bool = False) -> torch.Tensor:
         assert x_in.dtype == torch.float32 and x_in.is_contiguous() and x_in.shape == (S * T, self.cfg.d_model)
-        out = torch.empty_like(x_in)
+        out = self._empty(x_in.shape, torch.float32)
         arr = self._array(kv)
         kvl = ClaspKvLayer(arr[layer].k, arr[layer].v)
         _check(self.lib.clasp_layer_forward(self.handle, layer, x_in.data_ptr(), x_in.shape[1], S, T, ctx_len,
@@ -327,7 +347,7 @@ class Clasp:
     def gemm_xwT(self, x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
         R, K = x.shape
         N = w.shape[0]
-        y = torch.empty((R, N), dtype=torch.float32, device=self.device)
+        y = self._empty((R, N), torch.float32)
         _check(self.lib.clasp_gemm_xwT(self.handle, x.data_ptr(), w.data_ptr(), R, N, K, y.data_ptr()),
                "clasp_gemm_xwT")
         return y
@@ -342,12 +362,6 @@ class Clasp:
         if (sd != 1 or (sh != hd and heads > 1)) and shape[0]:
             raise ValueError(f"{what}: the heads of a row must be contiguous")
         return sr if shape[0] > 1 else heads * hd      # (nothing steps over a single row's stride)
-
-    def _new_rows(self, t: torch.Tensor) -> torch.Tensor:
-        # memory handed out for another stream than the one that fills it
-        if torch._C._cuda_getCurrentRawStream(self._index) != self._stream_ptr:
-            t.record_stream(self.stream)
-        return t
 
     def _kv4_layer(self, kv: KV4Cache, layer: int):
         if type(kv) is not KV4Cache and not isinstance(kv, KV4Cache) or kv.layout != self._layout:
@@ -378,11 +392,11 @@ class Clasp:
             raise ClaspError(-3, "clasp_kv4_read")      # (before memory for the rows is asked for)
         if k_out is None and v_out is None:
             shape = (n, h, self._hd)
-            k_out, v_out = self._new_rows(self._like.new_empty(shape)), self._new_rows(self._like.new_empty(shape))
+            k_out, v_out = self._empty(shape), self._empty(shape)
             ks = vs = h * self._hd
         else:
-            k_out = self._new_rows(self._like.new_empty((n, h, self._hd))) if k_out is None else k_out
-            v_out = self._new_rows(self._like.new_empty((n, h, self._hd))) if v_out is None else v_out
+            k_out = self._empty((n, h, self._hd)) if k_out is None else k_out
+            v_out = self._empty((n, h, self._hd)) if v_out is None else v_out
             ks, vs = self._head_rows(k_out, h, "k_out"), self._head_rows(v_out, h, "v_out")
             if k_out.shape[0] != n or v_out.shape[0] != n:
                 raise ValueError("k_out, v_out: n rows")
@@ -398,7 +412,8 @@ class Clasp:
         row that sees nothing gives zeros.  `out` must not overlap q."""
         h = self._nq
         qs = self._head_rows(q, h, "q")
-        R = q.shape[0]
+        shape = q.shape
+        R = shape[0]
         if T < 1 or R % T:
             raise ValueError("q: whole states of T rows")
         if visible is not None and (visible.dtype != torch.int32 or visible.device != q.device or visible.shape != (R,)
@@ -411,7 +426,7 @@ class Clasp:
         if not 0 <= ctx_len <= MAX_POSITION:
             raise ValueError("ctx_len: a number of positions")
         if out is None:
-            out, os = self._new_rows(torch.empty_like(q)), h * self._hd    # (rows with gaps give rows without)
+            out, os = self._empty(shape), h * self._hd
         else:
             os = self._head_rows(out, h, "out")
             if out.shape[0] != R:
