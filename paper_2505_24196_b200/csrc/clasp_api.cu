@@ -1559,7 +1559,7 @@ int clasp_layer_forward(clasp_ctx* ctx, int32_t layer, const float* x_in, int64_
   if (in_stride < ctx->cfg.d_model || out_stride < ctx->cfg.d_model) return CLASP_ERR_INVALID_ARG;
   if (!al16(x_in) || !al16(x_out) || (in_stride & 3) || (out_stride & 3) || !kv_aligned(kv_layer, 1))
     return CLASP_ERR_INVALID_ARG;
-  if ((int64_t)S * T > ctx->cfg.max_rows || ctx_len > ctx->cfg.max_ctx || pos0 + T > ctx->cfg.max_ctx)
+  if ((int64_t)S * T > ctx->cfg.max_rows || ctx_len > ctx->cfg.max_ctx || (int64_t)pos0 + T > ctx->cfg.max_ctx)
     return CLASP_ERR_CAPACITY;
   if (!ctx->loaded[layer]) return CLASP_ERR_NOT_LOADED;
   if (ctx->use_engine && S * T <= pk::MAX_ROWS && (!write_kv || pos0 == ctx_len)) {
