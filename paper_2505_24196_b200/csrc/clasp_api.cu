@@ -223,8 +223,8 @@ Workspace carve(const clasp_config& c, uint8_t* base) {
 cudaError_t kv4_attributes() {
   namespace k4 = clasp::kv4;
   const struct { const void* f; int bytes; } k[] = {
-      {(const void*)k4::attn_many_kernel<128, 1>, k4::many_smem<128, 1>()}, {(const void*)k4::attn_many_kernel<128, 2>, k4::many_smem<128, 2>()},
-      {(const void*)k4::attn_many_kernel<64, 1>, k4::many_smem<64, 1>()}, {(const void*)k4::attn_many_kernel<64, 2>, k4::many_smem<64, 2>()},
+      {(const void*)k4::attn_many_kernel<128, 1, false>, k4::many_smem<128, 1>()}, {(const void*)k4::attn_many_kernel<128, 2, false>, k4::many_smem<128, 2>()},
+      {(const void*)k4::attn_many_kernel<64, 1, false>, k4::many_smem<64, 1>()}, {(const void*)k4::attn_many_kernel<64, 2, false>, k4::many_smem<64, 2>()},
       {(const void*)k4::attn_rows_kernel<128, false>, k4::rows_smem<128, false>()}, {(const void*)k4::attn_rows_kernel<128, true>, k4::rows_smem<128, true>()},
       {(const void*)k4::attn_rows_kernel<64, false>, k4::rows_smem<64, false>()}, {(const void*)k4::attn_rows_kernel<64, true>, k4::rows_smem<64, true>()}};
   for (const auto& e : k) {
@@ -648,7 +648,9 @@ int kv4_many_launch(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
   const int items = p.blocks * p.nkv, keys = p.n_keys + (p.own_n > 0 ? std::min(p.own_n, NB * k4::TP + p.T) : 0);
   p.splits = std::max(1, std::min({ctx->num_sms / items, (keys + k4::TK - 1) / k4::TK, k4::MAX_SPLITS}));
   p.splits = std::min(p.splits, std::max(1, (int)(KV4_MANY_SLOTS / ((size_t)items * NB * k4::TP))));
-  k4::attn_many_kernel<HD, NB><<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
+  const auto kernel = ctx->wait_limit ? k4::attn_many_kernel<HD, NB, true> : k4::attn_many_kernel<HD, NB, false>;
+  if (ctx->wait_limit) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k4::many_smem<HD, NB>()));
+  kernel<<<items * p.splits, k4::many_threads<NB>(), k4::many_smem<HD, NB>(), ctx->stream>>>(p);
   int rc = launch_check(ctx);
   if (rc || p.splits == 1) return rc;
   if (p.splits <= 3) return kv4_merge<HD, NB, 3>(ctx, p);
@@ -672,7 +674,7 @@ int kv4_attend(clasp_ctx* ctx, clasp::kv4::AttnArgs p) {
     p.R = p.R_all;
     p.r0 = 0;
     p.status = ctx->ws.status;
-    p.spin_fast = ctx->wait_limit ? std::min(ctx->wait_limit, clasp::tc::SPIN_FAST) : clasp::tc::SPIN_FAST;
+    p.spin_fast = clasp::tc::SPIN_FAST;
     p.spin_slow = ctx->wait_limit ? ctx->wait_limit : clasp::tc::SPIN_SLOW;
     // One block of pairs per CTA where that gives every block an SM of its own and there is nothing to gain from sharing tiles: the
     // blocks need no parts, or the keys are few (400 rows of 32 heads 13.9 us, two blocks per CTA in two parts 20; 200 rows over

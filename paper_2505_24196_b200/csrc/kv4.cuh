@@ -311,7 +311,7 @@ struct AttnArgs {
   float2* part_ml;         // [R * nq, parts] (maximum, sum)
   int* counters;           // one per (kv head, block of pairs), zero on entry and on exit
   int* status;             // set when a bounded wait of attn_many_kernel runs out
-  uint32_t spin_fast, spin_slow;
+  uint32_t spin_fast, spin_slow;   // its polls (constants in their place unroll the loop: 4 % of a call)
   int blocks, splits;      // attn_many_kernel: blocks of pairs per kv head, parts of each block's key tiles
   int r0;                  // first row of this launch (of `visible` and the causal limit; q, out are offset already)
   int R_all;               // rows of the call
@@ -910,7 +910,9 @@ static_assert(sizeof(ManyShared) <= 2048, "fits its share of shared memory");
 // two warps per scheduler in step.  No gain from a quarter of the exponentials on the multiply-add pipe, from exponentials with
 // the previous maximum while the new one is found, nor from starting the blocks half a tile apart (51.8, 55.3, 56.8 us against
 // 51.4 then).
-template <int HD, int NB>
+//
+// LIMITED: for calls under a wait limit of the caller's.
+template <int HD, int NB, bool LIMITED>
 __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const __grid_constant__ AttnArgs p) {
   constexpr int NH = HD / 64;                        // 64-dim halves of a row
   constexpr uint32_t Q_BYTES = TP * HD * 2, KV_BYTES = TK * HD * 2, HALF_Q = TP * 128, HALF_KV = TK * 128;
@@ -970,11 +972,19 @@ __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const 
   const int t_lo = (int)((long long)nt_all * split / p.splits), nt = (int)((long long)nt_all * (split + 1) / p.splits) - t_lo;
 
   // A wait of a whole warp.  The first poll stands outside the bounded loop: most waits here find their phase complete, and the
-  // loop's code cost each of them about 200 cycles of the tile's chain.
+  // loop's code cost each of them about 200 cycles of the tile's chain.  Such a poll may suspend the warp for microseconds, in which a
+  // healthy wait is over: under a limit a poll is one look, some 100 ns with the sleep behind it.
   bool ok = true;
   auto warp_wait = [&](uint64_t* bar, uint32_t parity) {
-    if (!__all_sync(0xffffffffu, tc::mbar_test(tc::smem_u32(bar), parity))) {
-      ok = tc::mbar_wait(tc::smem_u32(bar), parity, p.status, p.spin_fast, p.spin_slow);
+    const uint32_t at = tc::smem_u32(bar);
+    if (!__all_sync(0xffffffffu, LIMITED ? tc::mbar_look(at, parity) : tc::mbar_test(at, parity))) {
+      if constexpr (LIMITED) {
+        ok = false;
+        for (uint32_t i = 0; i < p.spin_slow && !(ok = tc::mbar_look(at, parity)); ++i) __nanosleep(64);
+        if (!ok) atomicExch(p.status, 1);
+      } else {
+        ok = tc::mbar_wait(at, parity, p.status, p.spin_fast, p.spin_slow);
+      }
       ok = __all_sync(0xffffffffu, ok);
     }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
