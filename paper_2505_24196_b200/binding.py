@@ -256,10 +256,13 @@ class Clasp:
         _check(self.lib.clasp_load_head(self.handle, head["embed"].data_ptr(), head["final_norm"].data_ptr(),
                                         head["lm_head"].data_ptr()), "clasp_load_head")
 
+    def _is_current(self) -> bool:
+        return torch._C._cuda_getCurrentRawStream(self._index) == self._stream_ptr
+
     def _empty(self, shape, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
         """Memory for a result (model dtype if none is given).  It comes from the pool of the context's stream, in whose order it is
         written: a block of the current stream's pool may still be in use by what that stream has queued."""
-        if torch._C._cuda_getCurrentRawStream(self._index) == self._stream_ptr:
+        if self._is_current():
             return self._like.new_empty(shape) if dtype is None else self._like.new_empty(shape, dtype=dtype)
         with torch.cuda.stream(self.stream):
             t = self._like.new_empty(shape, dtype=dtype)
@@ -412,8 +415,7 @@ class Clasp:
         row that sees nothing gives zeros.  `out` must not overlap q."""
         h = self._nq
         qs = self._head_rows(q, h, "q")
-        shape = q.shape
-        R = shape[0]
+        R = q.shape[0]
         if T < 1 or R % T:
             raise ValueError("q: whole states of T rows")
         if visible is not None and (visible.dtype != torch.int32 or visible.device != q.device or visible.shape != (R,)
@@ -426,7 +428,9 @@ class Clasp:
         if not 0 <= ctx_len <= MAX_POSITION:
             raise ValueError("ctx_len: a number of positions")
         if out is None:
-            out, os = self._empty(shape), h * self._hd
+            # (empty_like is the quicker one, 1.2 us of a call's 8; rows with gaps give rows without)
+            out = torch.empty_like(q) if self._is_current() else self._empty(q.shape)
+            os = h * self._hd
         else:
             os = self._head_rows(out, h, "out")
             if out.shape[0] != R:
