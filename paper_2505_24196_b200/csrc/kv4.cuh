@@ -90,18 +90,6 @@ __device__ __forceinline__ void load16(const float* p, float (&x)[BLOCK]) {
     x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
   }
 }
-__device__ __forceinline__ void load16(const bf16* p, float (&x)[BLOCK]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      x[8 * i + 2 * k] = __uint_as_float(u[k] << 16);
-      x[8 * i + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
-    }
-  }
-}
 __device__ __forceinline__ void store16(float* p, const float (&x)[BLOCK]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -914,7 +902,6 @@ static_assert(sizeof(ManyShared) <= 2048, "fits its share of shared memory");
 // LIMITED: for calls under a wait limit of the caller's.
 template <int HD, int NB, bool LIMITED>
 __global__ void __launch_bounds__(many_threads<NB>(), 1) attn_many_kernel(const __grid_constant__ AttnArgs p) {
-  constexpr int NH = HD / 64;                        // 64-dim halves of a row
   constexpr uint32_t Q_BYTES = TP * HD * 2, KV_BYTES = TK * HD * 2, HALF_Q = TP * 128, HALF_KV = TK * 128;
   constexpr uint32_t TM_COLS = NB == 2 ? 512 : 256, O_COL = NB * 128;
   extern __shared__ __align__(1024) uint8_t smem[];
