@@ -292,7 +292,7 @@ int clasp_layer_forward(clasp_ctx* ctx, int32_t layer, const float* x_in, int64_
  * Format.  A block is 16 consecutive dims of one position's key or value, sixteen 4-bit codes c and one scale byte b:
  *     value = (c - 8) * s,   s = the half-precision number with the bits b << 7
  * Written: s the smallest such number with 7 s >= the block's largest magnitude (at most 896: magnitudes above 6272
- * saturate), c - 8 = x / s to the nearest, ties to even.  A block that holds an infinity or NaN gets b = 0xFF and reads
+ * saturate), c - 8 = x / s to the nearest, ties to even (a block with no magnitude above 2^-18 becomes zeros).  A block that holds an infinity or NaN gets b = 0xFF and reads
  * back as NaN throughout.  The bytes are a function of the row alone; every value is exact in bf16.  The array of one
  * layer's keys (or values): codes [n_kv_heads, max_ctx, head_dim / 2], low nibble first, then scale bytes
  * [n_kv_heads, max_ctx, head_dim / 16]; 16-byte aligned.  max_ctx is at most 2^30, n_kv_heads 2^14.

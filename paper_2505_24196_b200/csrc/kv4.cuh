@@ -7,7 +7,8 @@
 // correctly rounded quotient never reaches a border that x / s does not), so the bytes are a function of the row alone.  A
 // value has at most 8 significant bits: exact in bf16 and in half precision.  Sixteen dims per scale: uniform steps of
 // a seventh of a block's largest magnitude leave a Gaussian row 9.3 % of its standard deviation as error (4-bit floating point
-// with the same scale byte 10.0 %).  A block that holds an infinity or NaN gets the byte 0xFF and reads back as NaN throughout.
+// with the same scale byte 10.0 %).  A block that holds an infinity or NaN gets the byte 0xFF and reads back as NaN throughout; one
+// whose largest magnitude is 2^-18 or less, half the smallest scale, becomes zeros.
 //
 // One layer's array (keys or values): codes [n_kv, capacity, hd / 2], low nibble first, then scale bytes
 // [n_kv, capacity, hd / 16].  Head-major: what one CTA of the attention reads is contiguous.
@@ -235,8 +236,9 @@ __global__ void __launch_bounds__(256) read_kernel(View ck, View cv, int n, long
   }
 }
 
-// A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated and stored in the model dtype, keys rotated and
-// quantised, values quantised.  Dims i and i + hd / 2 share a rotation, so a thread of the rotated part takes the blocks j and j + hd / 32.
+// A layer's fused projections [R, (nq + 2 nkv) hd] (fp32): queries rotated and stored in the model dtype (in bf16 models rounded to
+// its 8 bits, as the persistent kernel rounds them: the multiplies take bf16 or half precision), keys rotated and quantised,
+// values quantised.  Dims i and i + hd / 2 share a rotation, so a thread of the rotated part takes the blocks j and j + hd / 32.
 template <typename T>
 __global__ void __launch_bounds__(256) store_rows_kernel(const float* __restrict__ qkv, long long ld, const float2* __restrict__ cs, int R,
                                                          int rows, int nq, int nkv, int hd, View ck, View cv, long long pos0,
@@ -439,13 +441,15 @@ template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const vo
 // half precision.  q is scaled by a power of two per row to a largest magnitude in [2^9, 2^10) (a nibble's 16 on top of it, see
 // nib_lo) and rounded to half precision: exact for bf16 rows (what lies 2^25 below the row's maximum aside); SPLIT (fp32 models)
 // adds the rounding error of q and of the weights as a second half-precision operand: 22 bits.  Weights: half precision of 2^12 exp2(s - m), m a maximum that moves
-// only when exceeded by 2^3, so they stay below 2^15 and lose nothing above 2^-26 of the largest; sums in fp32.
+// only when exceeded by 2^3, so they stay below 2^15 and lose nothing above 2^-26 of the largest; sums in fp32.  One part, 11 bits, is
+// enough for bf16 results of 8: their error against 64 bits is 0.5 % above that of fp32 weights (1.648e-3 against 1.641e-3 over 512
+// positions), a second part would double these multiplies.
 // A block with the NaN byte must reach only the rows that see it, and 0 x NaN is NaN: values' NaN blocks enter as zeros, and
 // `poison` remembers which (pair, block) they belong to.
 //
-// Measured, eight kv heads of 128, us: one token over 512 / 131071 positions (four pairs) 7.2 / 39.3, five rows of 64 heads over
-// 2048 12.6.  A step is about 300 instructions and 1850 cycles of sixteen warps side by side (64 % of the issue slots, the
-// conversion's logic and half-precision pipes at 47 %): 131071 positions move at 3.9 TB/s.  Straight loads of a step one ahead
+// Measured, eight kv heads of 128, us: one token over 512 / 131071 positions (four pairs) 7.2 / 38.9, five rows of 64 heads over
+// 2048 12.5.  A step is about 300 instructions and 1850 cycles of sixteen warps side by side (61 % of the issue slots, the
+// conversion's logic and half-precision pipes at 48 and 38 %): 131071 positions move at 3.9 TB/s.  Straight loads of a step one ahead
 // took 55.7 us, twenty or twenty-four warps 42.0 / 44.7, sixteen pairs per CTA as long per pair (17 instead of 12.6 us for the
 // five rows).  Below a thousand positions it is launch, first instruction fetches and the joining of the warps.
 template <int HD, bool SPLIT>
@@ -890,7 +894,8 @@ static_assert(sizeof(ManyShared) <= 2048, "fits its share of shared memory");
 //   tcgen05, S / P / O in tensor memory
 // A thread owns a pair; its maximum moves only when exceeded by 2^5 (then O is rescaled).  Scores are double-buffered: the next
 // tile's Q K^T runs under this tile's softmax.  NaN blocks: as in attn_rows_kernel; where a value's NaN block was met, the pairs
-// look through the scale bytes of the keys they see once more at the end.
+// look through the scale bytes of the keys they see once more at the end.  Half-precision weights: as there (error against 64 bits 0.5 -
+// 0.7 % above that of fp32 weights).
 //
 // Measured, 32 query heads over eight kv heads of 128, us: a prompt of 1999 rows 49, 128 rows over 4095 positions 22.8 with its
 // merge, twelve states over 8192 19.4.  A tile of 2 x 128 pairs takes 2000 cycles where its multiplies take 1280 and its
